@@ -317,6 +317,116 @@ int hbl_kv_dequant(const void* packed, const float* scales, int64_t rows, int64_
                    void* out, int out_dtype, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Rotary positions, the paged cache of head states, and the attention that reads it
+ * (between the QKV projection and W_o: rotate and append, attend, project)
+ * ------------------------------------------------------------------------- */
+
+/* How rotated features pair up: i with i + rot_dim/2, or 2i with 2i + 1. */
+#define HBL_ROPE_HALF 0
+#define HBL_ROPE_INTERLEAVED 1
+
+/* Frequencies for contexts beyond the trained one. */
+#define HBL_ROPE_PLAIN 0    /* f_i = base^(-2i/rot_dim)                                                              */
+#define HBL_ROPE_LINEAR 1   /* f_i / factor                                                                          */
+#define HBL_ROPE_BASE 2     /* base * factor^(rot_dim/(rot_dim-2)) in place of base: the slowest pair slows by factor */
+#define HBL_ROPE_PARTS 3    /* with n_i = trained_len f_i / 2 pi turns over the trained context and
+                               g = clamp((n_i - slow)/(fast - slow), 0, 1):  f_i (g + (1 - g)/factor)                */
+/*
+ * Host only: freqs[0 .. rot_dim/2) in HOST memory, computed in fp64 and rounded once.  rot_dim even, 4 to 512; base > 1,
+ * factor >= 1; trained_len, slow and fast are read for HBL_ROPE_PARTS only (trained_len > 0, 0 <= slow < fast).
+ */
+int hbl_rope_frequencies(int64_t rot_dim, double base, int scaling, double factor, double trained_len, double slow,
+                         double fast, float* freqs);
+
+/*
+ * Rotary positions of head states, forward and backward.  Per token t, head h and pair (x1, x2), with
+ * angle = positions[t] * freqs[i] (a product in fp64, reduced to one turn) and m = magnitude:
+ *   backward == 0:  y1 = x1 (m cos) - x2 (m sin),  y2 = x2 (m cos) + x1 (m sin)
+ *   backward != 0:  the transposed map, which takes dL/dy to dL/dx: the same with -angle
+ * Features from rot_dim on are passed through.
+ *   x          [T, H, d], x_dtype; a token's heads are contiguous, x_stride values lie between two tokens (a slice of a
+ *              fused QKV output is taken where it is);  out likewise with out_dtype and out_stride.  out may be x itself
+ *              (same type and stride), and must not overlap it otherwise
+ *   positions  device [T] int32, any value;  freqs device [rot_dim/2] fp32
+ *   H >= 1, d a multiple of 16 up to 512, rot_dim a multiple of 16 up to d, strides >= H d and of whole 16 bytes
+ */
+int hbl_rope(const void* x, int x_dtype, int64_t T, int64_t H, int64_t d, int64_t x_stride, const int32_t* positions,
+             const float* freqs, int64_t rot_dim, int layout, float magnitude, int backward, void* out, int out_dtype,
+             int64_t out_stride, void* stream);
+
+/*
+ * A paged cache: two pools (keys and values) of n_pages pages of page_size slots.  Row (page p, head h, slot i) of a pool is
+ * row p * page_rows + h * page_size + i: d bf16 values (bits == 16), or d codes of 8, 4 or 3 bits as hbl_kv_quant_absmax
+ * writes them, with the row's scale at the same index of the scales.  hbl_kv_dequant reads a pool back.
+ *   k, v                device, 16-byte aligned;  k_scales, v_scales device fp32 (not read when bits == 16)
+ *   page_size           a power of two, 16 to 1024
+ *   page_rows           rows between two pages, >= n_kv_heads * page_size (more where pools are interleaved)
+ *   d                   64, 128 or 256
+ */
+typedef struct hbl_kv_cache {
+    void* k;
+    void* v;
+    float* k_scales;
+    float* v_scales;
+    int64_t n_pages, page_rows;
+    int bits, page_size, n_kv_heads, d;
+} hbl_kv_cache;
+
+/*
+ * A ragged batch of sequences over a cache, described by device arrays that the kernels read (the host never waits for them).
+ * Sequence s has the new tokens [q_starts[s], q_starts[s+1]) of the call, the last ones of its kv_lens[s] keys (counted with
+ * them): the new token q_starts[s] + i is at position kv_lens[s] - n + i, n being their number.  Key j lies in slot
+ * j mod page_size of page block_table[s * table_stride + j / page_size].
+ *   q_starts [n_seqs + 1] and kv_lens [n_seqs] int32, q_starts not decreasing;  block_table [n_seqs] rows of table_width
+ * An entry of the table outside [0, n_pages) stands for no page: nothing is written there, and its keys are left out of the
+ * attention (a window may have passed them).  Keys beyond table_width pages do not exist.  Tokens outside every sequence,
+ * [0, q_starts[0]) and [q_starts[n_seqs], T), are left as they were.
+ */
+typedef struct hbl_kv_batch {
+    const int32_t* q_starts;
+    const int32_t* kv_lens;
+    const int32_t* block_table;
+    int64_t table_stride;
+    int n_seqs, table_width;
+} hbl_kv_batch;
+
+/*
+ * Appends the new tokens' keys and values to the cache, the keys rotated to their positions on the way (as hbl_rope does, no
+ * rounding in between: low-bit codes and scales are those of hbl_kv_quant_absmax on the fp32 output of hbl_rope), and, where
+ * q is given, rotates the queries in the same launch.
+ *   k, v    [T, n_kv_heads, d] x_dtype, strides in values as for hbl_rope
+ *   q       [T, n_q_heads, d] x_dtype or NULL;  q_out likewise in q_out_dtype, may be q itself (same type and stride)
+ *   freqs   device [rot_dim/2] fp32, or NULL: no rotation (rot_dim, layout and magnitude are not read)
+ *   eps     of the quantiser (bits < 16)
+ * Two tokens that the table sends to one slot leave either's row there, and with bits < 16 maybe parts of both.
+ */
+int hbl_kv_append(const hbl_kv_cache* cache, const hbl_kv_batch* batch, const void* k, int64_t k_stride, const void* v,
+                  int64_t v_stride, int x_dtype, int64_t T, const void* q, int64_t n_q_heads, int64_t q_stride, void* q_out,
+                  int q_out_dtype, int64_t q_out_stride, const float* freqs, int64_t rot_dim, int layout, float magnitude,
+                  float eps, void* stream);
+
+/*
+ * Attention of the new tokens against the cache, their own keys included (append first): one token a sequence, a chunk, or
+ * both in one batch.  Query head h reads key head h / (n_q_heads / n_kv_heads).  With p the token's position and j a key's:
+ *   s_j = scale q.k_j;   softcap > 0:  s_j = softcap tanh(s_j / softcap);   slopes:  s_j -= slopes[h] |p - j|
+ *   visible: (j <= p, or j < prefix_lens[s]), and (window == 0, or j > p - window)
+ *   out = sum_j softmax(s)_j v_j over the visible keys;  zeros where there are none
+ * Scores, maxima, sums and outputs are held in fp32, products on the matrix cores with codes as exact integers; the softmax's
+ * weights are rounded to bf16 for the product with the values.
+ *   q, out          [T, n_q_heads, d] bf16 with strides in values as for hbl_rope; they must not overlap
+ *   max_q_len       at least the new tokens of any sequence (those beyond it are left as they were)
+ *   window >= 0;  slopes device [n_q_heads] fp32 or NULL;  prefix_lens device [n_seqs] int32 or NULL
+ *   workspace       device, >= hbl_paged_attention_workspace_bytes(same arguments), 256-byte aligned; nothing in it has to
+ *                   start at a value; calls that may overlap need one each
+ */
+size_t hbl_paged_attention_workspace_bytes(const hbl_kv_cache* cache, const hbl_kv_batch* batch, int64_t T, int64_t n_q_heads,
+                                           int64_t max_q_len);
+int hbl_paged_attention(const void* q, int64_t T, int64_t n_q_heads, int64_t q_stride, const hbl_kv_cache* cache,
+                        const hbl_kv_batch* batch, int64_t max_q_len, float scale, float softcap, int64_t window,
+                        const float* slopes, const int32_t* prefix_lens, void* out, int64_t out_stride, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Kernel timing (benchmarks and profiling; not part of the forward path)
  * ---------------------------------------------------------------------------
  * Between hbl_trace_begin and hbl_trace_end every kernel this library launches from the calling thread

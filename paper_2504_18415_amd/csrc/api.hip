@@ -1,8 +1,10 @@
 // C-ABI entry points of libhbitlinear: argument validation and kernel sequencing only.
+#include <cmath>
 #include <vector>
 
 #include "hbl_internal.h"
 #include "hbl_test_exports.h"
+#include "paged_attention.h"
 
 namespace hbl {
 
@@ -529,6 +531,187 @@ int hbl_test_gemm_i32_tile(const void* codes, int code_form, int64_t T, int64_t 
                                         nullptr, s, acc, tile);
     return launch_ternary_gemm(static_cast<const int8_t*>(codes), 0, T, K, Wq_packed, N, nullptr, nullptr, 1, nullptr,
                                acc, s, tile);
+}
+
+namespace {
+
+constexpr int64_t kMostTokens = 1 << 24, kMostValues = (int64_t)1 << 40;   // (values between two tokens times tokens)
+
+bool dtype_ok(int t) { return t == HBL_F32 || t == HBL_BF16; }
+int value_bytes(int t) { return t == HBL_BF16 ? 2 : 4; }
+
+// Head states [T, H, d] with `stride` values between two tokens.
+int check_heads(const void* x, int dtype, int64_t T, int64_t H, int64_t d, int64_t stride) {
+    if (stride < H * d || stride > kMostValues || T * stride > kMostValues) return HBL_E_SHAPE;
+    if (!x) return HBL_E_NULL;
+    if (!aligned16(x) || (stride * value_bytes(dtype)) % 16 != 0) return HBL_E_ALIGN;
+    return HBL_OK;
+}
+int check_rotation(int64_t rot_dim, int64_t d, int layout) {
+    if (layout != HBL_ROPE_HALF && layout != HBL_ROPE_INTERLEAVED) return HBL_E_SHAPE;
+    return rot_dim < 16 || rot_dim > d || rot_dim % 16 != 0 ? HBL_E_SHAPE : HBL_OK;
+}
+int check_cache(const hbl_kv_cache* c) {
+    if (!c) return HBL_E_NULL;
+    if (c->bits != 16 && c->bits != 8 && c->bits != 4 && c->bits != 3) return HBL_E_BITS;
+    if (c->d != 64 && c->d != 128 && c->d != 256) return HBL_E_SHAPE;
+    if (!is_pow2(c->page_size) || c->page_size < 16 || c->page_size > 1024) return HBL_E_SHAPE;
+    if (c->n_kv_heads < 1 || c->n_kv_heads > (1 << 16) || c->n_pages < 0 || c->n_pages > 0x7FFFFFFF) return HBL_E_SHAPE;
+    if (c->page_rows < (int64_t)c->n_kv_heads * c->page_size || c->page_rows > kMostValues / c->d ||
+        (c->n_pages > 0 && c->page_rows > kMostValues / c->d / c->n_pages))
+        return HBL_E_SHAPE;
+    return HBL_OK;
+}
+int check_cache_memory(const hbl_kv_cache* c) {
+    if (!c->k || !c->v || (c->bits != 16 && (!c->k_scales || !c->v_scales))) return HBL_E_NULL;
+    return aligned16(c->k) && aligned16(c->v) ? HBL_OK : HBL_E_ALIGN;
+}
+int check_batch(const hbl_kv_batch* b, int64_t T) {
+    if (!b) return HBL_E_NULL;
+    if (T < 0 || T > kMostTokens || b->n_seqs < 0 || b->n_seqs > (1 << 20) || b->table_width < 0 || b->table_stride < b->table_width)
+        return HBL_E_SHAPE;
+    if (b->table_width > (1 << 26) || b->table_stride > kMostValues) return HBL_E_SHAPE;
+    return HBL_OK;
+}
+int check_batch_memory(const hbl_kv_batch* b) {
+    return b->q_starts && b->kv_lens && (b->block_table || b->table_width == 0) ? HBL_OK : HBL_E_NULL;
+}
+PagedCache paged_cache(const hbl_kv_cache* c) {
+    int shift = 0;
+    while ((1 << shift) < c->page_size) ++shift;
+    return {static_cast<uint8_t*>(c->k), static_cast<uint8_t*>(c->v), c->k_scales, c->v_scales, c->page_rows, (int)c->n_pages, c->n_kv_heads, shift};
+}
+PagedBatch paged_batch(const hbl_kv_batch* b) {
+    return {b->q_starts, b->kv_lens, b->block_table, b->table_stride, b->n_seqs, b->table_width};
+}
+// Sizes of an attention call (nothing here is read through a pointer).
+int check_attention_shape(const hbl_kv_cache* c, const hbl_kv_batch* b, int64_t T, int64_t Hq, int64_t max_q_len) {
+    int rc = check_cache(c);
+    if (rc == HBL_OK) rc = check_batch(b, T);
+    if (rc != HBL_OK) return rc;
+    if (Hq < 1 || Hq > (1 << 16) || Hq % c->n_kv_heads != 0 || max_q_len < 1) return HBL_E_SHAPE;
+    return HBL_OK;
+}
+
+}  // namespace
+
+int hbl_rope_frequencies(int64_t rot_dim, double base, int scaling, double factor, double trained_len, double slow, double fast,
+                         float* freqs) {
+    if (rot_dim < 4 || rot_dim > 512 || rot_dim % 2 != 0 || !(base > 1.0) || !(factor >= 1.0) || std::isinf(base) || std::isinf(factor))
+        return HBL_E_SHAPE;
+    if (scaling < HBL_ROPE_PLAIN || scaling > HBL_ROPE_PARTS) return HBL_E_SHAPE;
+    if (scaling == HBL_ROPE_PARTS && (!(trained_len > 0.0) || !(slow >= 0.0) || !(fast > slow))) return HBL_E_SHAPE;
+    if (!freqs) return HBL_E_NULL;
+    if (scaling == HBL_ROPE_BASE) base *= std::pow(factor, (double)rot_dim / (double)(rot_dim - 2));
+    for (int64_t i = 0; i < rot_dim / 2; ++i) {
+        double f = std::pow(base, -2.0 * (double)i / (double)rot_dim);
+        if (scaling == HBL_ROPE_LINEAR) f /= factor;
+        if (scaling == HBL_ROPE_PARTS) {
+            const double n = trained_len * f / 6.283185307179586477;
+            const double g = std::fmin(1.0, std::fmax(0.0, (n - slow) / (fast - slow)));
+            f *= g + (1.0 - g) / factor;
+        }
+        freqs[i] = (float)f;
+    }
+    return HBL_OK;
+}
+
+int hbl_rope(const void* x, int x_dtype, int64_t T, int64_t H, int64_t d, int64_t x_stride, const int32_t* positions,
+             const float* freqs, int64_t rot_dim, int layout, float magnitude, int backward, void* out, int out_dtype,
+             int64_t out_stride, void* stream) {
+    if (!dtype_ok(x_dtype) || !dtype_ok(out_dtype)) return HBL_E_DTYPE;
+    if (T < 0 || T > kMostTokens || H < 1 || H > (1 << 16) || d < 16 || d > 512 || d % 16 != 0) return HBL_E_SHAPE;
+    int rc = check_rotation(rot_dim, d, layout);
+    if (rc != HBL_OK) return rc;
+    if (T == 0) return HBL_OK;
+    rc = check_heads(x, x_dtype, T, H, d, x_stride);
+    if (rc == HBL_OK) rc = check_heads(out, out_dtype, T, H, d, out_stride);
+    if (rc != HBL_OK) return rc;
+    if (!positions || !freqs) return HBL_E_NULL;
+    if (x == out && (x_dtype != out_dtype || x_stride != out_stride)) return HBL_E_SHAPE;
+    return launch_rope(x, x_dtype, T, H, d, x_stride, positions, freqs, rot_dim, layout, magnitude, backward != 0, out, out_dtype,
+                       out_stride, static_cast<hipStream_t>(stream));
+}
+
+int hbl_kv_append(const hbl_kv_cache* cache, const hbl_kv_batch* batch, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                  int x_dtype, int64_t T, const void* q, int64_t n_q_heads, int64_t q_stride, void* q_out, int q_out_dtype,
+                  int64_t q_out_stride, const float* freqs, int64_t rot_dim, int layout, float magnitude, float eps, void* stream) {
+    int rc = check_cache(cache);
+    if (rc == HBL_OK) rc = check_batch(batch, T);
+    if (rc != HBL_OK) return rc;
+    if (!dtype_ok(x_dtype) || (q && !dtype_ok(q_out_dtype))) return HBL_E_DTYPE;
+    if (freqs && (rc = check_rotation(rot_dim, cache->d, layout)) != HBL_OK) return rc;
+    if (q && (n_q_heads < 1 || n_q_heads > (1 << 16))) return HBL_E_SHAPE;
+    if (T == 0 || batch->n_seqs == 0) return HBL_OK;
+    if ((rc = check_cache_memory(cache)) != HBL_OK || (rc = check_batch_memory(batch)) != HBL_OK) return rc;
+    if ((rc = check_heads(k, x_dtype, T, cache->n_kv_heads, cache->d, k_stride)) != HBL_OK) return rc;
+    if ((rc = check_heads(v, x_dtype, T, cache->n_kv_heads, cache->d, v_stride)) != HBL_OK) return rc;
+    if (q) {
+        if ((rc = check_heads(q, x_dtype, T, n_q_heads, cache->d, q_stride)) != HBL_OK) return rc;
+        if ((rc = check_heads(q_out, q_out_dtype, T, n_q_heads, cache->d, q_out_stride)) != HBL_OK) return rc;
+        if (q == q_out && (x_dtype != q_out_dtype || q_stride != q_out_stride)) return HBL_E_SHAPE;
+    }
+    return launch_kv_append(paged_cache(cache), cache->bits, cache->d, paged_batch(batch), k, k_stride, v, v_stride, x_dtype, T, q,
+                            n_q_heads, q_stride, q_out, q_out_dtype, q_out_stride, freqs, rot_dim, layout, magnitude, eps,
+                            static_cast<hipStream_t>(stream));
+}
+
+size_t hbl_paged_attention_workspace_bytes(const hbl_kv_cache* cache, const hbl_kv_batch* batch, int64_t T, int64_t n_q_heads,
+                                           int64_t max_q_len) {
+    if (check_attention_shape(cache, batch, T, n_q_heads, max_q_len) != HBL_OK) return 0;
+    return paged_attention_workspace(T, batch->n_seqs, (int)n_q_heads, cache->n_kv_heads, cache->d, max_q_len);
+}
+
+int hbl_paged_attention(const void* q, int64_t T, int64_t n_q_heads, int64_t q_stride, const hbl_kv_cache* cache,
+                        const hbl_kv_batch* batch, int64_t max_q_len, float scale, float softcap, int64_t window, const float* slopes,
+                        const int32_t* prefix_lens, void* out, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                        void* stream) {
+    int rc = check_attention_shape(cache, batch, T, n_q_heads, max_q_len);
+    if (rc != HBL_OK) return rc;
+    if (window < 0 || window > 0x7FFFFFFF || !(softcap >= 0.0f) || std::isinf(softcap) || !std::isfinite(scale)) return HBL_E_SHAPE;
+    if (T == 0 || batch->n_seqs == 0) return HBL_OK;
+    if ((rc = check_cache_memory(cache)) != HBL_OK || (rc = check_batch_memory(batch)) != HBL_OK) return rc;
+    if ((rc = check_heads(q, HBL_BF16, T, n_q_heads, cache->d, q_stride)) != HBL_OK) return rc;
+    if ((rc = check_heads(out, HBL_BF16, T, n_q_heads, cache->d, out_stride)) != HBL_OK) return rc;
+    if (!workspace) return HBL_E_NULL;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return HBL_E_ALIGN;
+    if (workspace_bytes < paged_attention_workspace(T, batch->n_seqs, (int)n_q_heads, cache->n_kv_heads, cache->d, max_q_len))
+        return HBL_E_WORKSPACE;
+    AttentionArgs a{};
+    a.q = static_cast<const uint16_t*>(q);
+    a.out = static_cast<uint16_t*>(out);
+    a.q_stride = q_stride;
+    a.out_stride = out_stride;
+    a.cache = paged_cache(cache);
+    a.batch = paged_batch(batch);
+    a.slopes = slopes;
+    a.prefix_lens = prefix_lens;
+    a.scale = scale;
+    a.softcap = softcap;
+    a.T = (int)T;
+    a.group = (int)(n_q_heads / cache->n_kv_heads);
+    a.d = cache->d;
+    a.window = (int)window;
+    return launch_paged_attention(a, cache->bits, max_q_len, workspace, static_cast<hipStream_t>(stream));
+}
+
+int hbl_test_kv_rows(const hbl_kv_cache* cache, const hbl_kv_batch* batch, int64_t T, int seq, int64_t* rows, int n_rows, int* span) {
+    const PagedCache c = paged_cache(cache);
+    const PagedBatch b = paged_batch(batch);
+    const SeqSpan s = span_of(b, c.page_shift, (int)T, seq);
+    span[0] = s.first;
+    span[1] = s.n;
+    span[2] = s.keys;
+    span[3] = s.total;
+    for (int j = 0; j < n_rows; ++j) rows[j] = j < s.keys ? key_row(c, b, seq, j, cache->n_kv_heads - 1) : -2;
+    return HBL_OK;
+}
+
+int hbl_test_visible_keys(int position, int keys, int window, int prefix, int* lo, int* hi) {
+    const KeyRange r = visible_keys(position, keys, window, prefix);
+    *lo = r.lo;
+    *hi = r.hi;
+    return HBL_OK;
 }
 
 int hbl_trace_begin(int max_launches) {

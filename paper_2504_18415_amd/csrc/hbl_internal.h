@@ -10,6 +10,7 @@
 
 #include "code_records.h"
 #include "hbitlinear.h"
+#include "paged.h"
 
 namespace hbl {
 
@@ -148,6 +149,14 @@ int launch_kv_quant(const void* x, int x_dtype, int64_t rows, int64_t d, int bit
                     float* scales, hipStream_t stream);
 int launch_kv_dequant(const void* packed, const float* scales, int64_t rows, int64_t d, int bits, void* out,
                       int out_dtype, hipStream_t stream);
+// Rotary positions and the paged cache (rope.hip; the attention that reads it: paged_attention.h)
+int launch_rope(const void* x, int x_dtype, int64_t T, int64_t H, int64_t d, int64_t x_stride, const int32_t* positions,
+                const float* freqs, int64_t rot_dim, int layout, float magnitude, bool backward, void* out, int out_dtype,
+                int64_t out_stride, hipStream_t stream);
+int launch_kv_append(const PagedCache& cache, int bits, int d, const PagedBatch& batch, const void* k, int64_t k_stride, const void* v,
+                     int64_t v_stride, int x_dtype, int64_t T, const void* q, int64_t Hq, int64_t q_stride, void* q_out, int q_out_dtype,
+                     int64_t q_out_stride, const float* freqs, int64_t rot_dim, int layout, float magnitude, float eps,
+                     hipStream_t stream);
 int launch_fwht_only(const void* x, int x_dtype, int64_t T, int64_t K, void* out, int out_dtype, hipStream_t stream);
 
 // Workgroup tiles of the two prefill GEMM kernels.  kTileAuto is the choice every forward call makes from the

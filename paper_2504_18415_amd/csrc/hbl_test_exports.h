@@ -50,6 +50,15 @@ int hbl_test_gemm_tile(int64_t T, int64_t K, int64_t N, int code_form);
 int hbl_test_gemm_i32_tile(const void* codes, int code_form, int64_t T, int64_t K, const void* Wq_packed,
                            int64_t N, int32_t* acc, int tile, void* stream);
 
+/*
+ * Host only, the batch's arrays in HOST memory: how the kernels of the paged cache read sequence `seq` - span[4] = first token,
+ * new tokens, keys, length as given - and the pool rows of its first n_rows keys for the last head (-1: no page, -2: no key).
+ */
+int hbl_test_kv_rows(const hbl_kv_cache* cache, const hbl_kv_batch* batch, int64_t T, int seq, int64_t* rows, int n_rows,
+                     int* span);
+/* Host only: the keys [lo, hi) that a token sees. */
+int hbl_test_visible_keys(int position, int keys, int window, int prefix, int* lo, int* hi);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,14 +11,10 @@
 // of a row at bits [b*i, b*i+b)): a thread's 8 codes are 8, 4 or 3 bytes; at 3 bits the four lanes of a quad
 // merge their 24-bit pieces into three dwords so that every store is an aligned dword.
 #include "hbl_internal.h"
+#include "kv_codes.h"
 
 namespace hbl {
 namespace {
-
-__device__ __forceinline__ float as_f(uint32_t u) { return __builtin_bit_cast(float, u); }
-__device__ __forceinline__ uint32_t as_u(float f) { return __builtin_bit_cast(uint32_t, f); }
-
-constexpr float kMagic = 12582912.0f;   // 1.5 * 2^23: adding it rounds to an integer (nearest-even)
 
 template <int CTRL>
 __device__ __forceinline__ uint32_t quad_lane(uint32_t v) {   // value of one fixed lane of the quad
@@ -79,16 +75,9 @@ __global__ __launch_bounds__(256) void kv_quant_kernel(const void* __restrict__ 
         for (int i = 0; i < 8; ++i) gamma = fmaxf(gamma, fabsf(h[i]));
         for (int m = 1; m < (1 << log2_lanes); m <<= 1) gamma = fmaxf(gamma, __shfl_xor(gamma, m, 64));
 
-        constexpr int half = 1 << (BITS - 1);
-        constexpr float qmax = (float)(half - 1);
-        const float s_q = qmax / (gamma + eps);
-        if (live && (t & ((1 << log2_lanes) - 1)) == 0) scales[t >> log2_lanes] = gamma / qmax;
-
-        // t + (1.5*2^23 + half): the fp32 adder rounds to nearest even and leaves code + half in the low mantissa bits
+        if (live && (t & ((1 << log2_lanes) - 1)) == 0) scales[t >> log2_lanes] = kv_scale<BITS>(gamma);
         uint32_t u[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            u[i] = as_u(__builtin_amdgcn_fmed3f(h[i] * s_q, -(float)half, qmax) + (kMagic + (float)half)) & 0xFFu;
+        kv_codes8<BITS>(h, kv_gain<BITS>(gamma, eps), u);
 
         if constexpr (BITS == 8) {
             if (live)

@@ -1,0 +1,309 @@
+// Rotary positions, and the appending of keys and values to a paged cache with that rotation applied on the way.
+//
+// Rotation of a head: pair i (features i and i + r/2, or 2i and 2i + 1, of the first r) turns by angle position * freqs[i],
+//   y1 = x1 (m cos) - x2 (m sin),   y2 = x1 (m sin) + x2 (m cos);   features from r on pass.
+// The transposed map (the gradient's) is the same with -angle.  The angle is a product in fp64 reduced to a part of one turn before it
+// becomes fp32: at position 10^6 an fp32 product would be off by 0.03 rad.
+//
+// Memory-bound streaming kernels: every value is read once and written once.  A workgroup first puts the r/2 factors of each of its
+// tokens into LDS, one per thread (an fp64 product and a sincospif: done per value they would cost as much as the traffic), then its
+// threads take 16 values of a head each: two pieces of 8, the two sides of 8 pairs, so that a rotation needs no other lane.
+#include "hbl_internal.h"
+#include "kv_codes.h"
+#include "paged.h"
+
+namespace hbl {
+namespace {
+
+constexpr int kThreads = 256;
+
+// 8 values as they are loaded
+template <bool BF16>
+struct Raw {
+    uint4 w[BF16 ? 1 : 2];
+};
+template <bool BF16>
+__device__ __forceinline__ Raw<BF16> load8(const void* x, int64_t at) {   // at: in values, a multiple of 8
+    Raw<BF16> r;
+    if constexpr (BF16) {
+        r.w[0] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(x) + at);
+    } else {
+        const uint4* p = reinterpret_cast<const uint4*>(static_cast<const float*>(x) + at);
+        r.w[0] = p[0];
+        r.w[1] = p[1];
+    }
+    return r;
+}
+template <bool BF16>
+__device__ __forceinline__ void widen8(const Raw<BF16>& r, float* v) {
+    const uint32_t w[4] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w};
+    if constexpr (BF16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = as_f(w[i] << 16);
+            v[2 * i + 1] = as_f(w[i] & 0xFFFF0000u);
+        }
+    } else {
+        const uint32_t u[4] = {r.w[1].x, r.w[1].y, r.w[1].z, r.w[1].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = as_f(w[i]);
+            v[4 + i] = as_f(u[i]);
+        }
+    }
+}
+template <bool BF16>
+__device__ __forceinline__ void store8(void* out, int64_t at, const float* v) {
+    if constexpr (BF16) {
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at) = pack_bf16x8(v);
+    } else {
+        float4* p = reinterpret_cast<float4*>(static_cast<float*>(out) + at);
+        p[0] = make_float4(v[0], v[1], v[2], v[3]);
+        p[1] = make_float4(v[4], v[5], v[6], v[7]);
+    }
+}
+
+struct Rotation {
+    const float* freqs;   // [pairs]; nullptr: no rotation (pairs is 0)
+    int pairs;            // r / 2, a multiple of 8
+    int interleaved;
+    float magnitude;      // m
+    float sign;           // -1: transposed
+};
+
+__device__ __forceinline__ float2 turn(const Rotation& r, int position, int i) {
+    const double turns = (double)position * (double)r.freqs[i] * 0.15915494309189533577;   // / 2 pi
+    float s, c;
+    sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
+    return make_float2(r.magnitude * c, r.sign * r.magnitude * s);
+}
+
+// Thread j of a head holds the pieces (of 8 values) first and second: in the rotated part the two sides of pairs 8j .. 8j + 7.
+struct Pieces {
+    int first, second;
+};
+__device__ __forceinline__ Pieces pieces_of(const Rotation& r, int j) {
+    const int half = r.pairs >> 3;
+    if (!r.interleaved && j < half) return {j, j + half};
+    return {2 * j, 2 * j + 1};
+}
+// (separate products and one rounding each, as the formula is written: codes made of the result do not depend on the call)
+__device__ __forceinline__ void rotate16(const Rotation& r, const float2* turns, int j, float* a, float* b) {
+    if (8 * j >= r.pairs) return;
+    const float2* t = turns + 8 * j;
+    if (r.interleaved) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 u = t[i], w = t[4 + i];
+            const float x = a[2 * i], y = a[2 * i + 1], p = b[2 * i], q = b[2 * i + 1];
+            a[2 * i] = x * u.x - y * u.y;
+            a[2 * i + 1] = x * u.y + y * u.x;
+            b[2 * i] = p * w.x - q * w.y;
+            b[2 * i + 1] = p * w.y + q * w.x;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 u = t[i];
+            const float x = a[i], y = b[i];
+            a[i] = x * u.x - y * u.y;
+            b[i] = x * u.y + y * u.x;
+        }
+    }
+}
+
+// --- rotation alone --------------------------------------------------------------------------------------------
+
+struct RopeArgs {
+    const void* x;
+    void* out;
+    const int32_t* positions;
+    int64_t x_stride, out_stride;   // values between two tokens
+    int T, H, d, tokens;            // tokens a workgroup
+    Rotation rot;
+};
+
+template <bool BF16, bool BF16OUT>
+__global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
+    extern __shared__ float2 turns[];   // [tokens][pairs]
+    const int t0 = (int)blockIdx.x * a.tokens;
+    const int n = a.T - t0 < a.tokens ? a.T - t0 : a.tokens;
+    for (int i = threadIdx.x; i < n * a.rot.pairs; i += kThreads) {
+        const int t = i / a.rot.pairs;
+        turns[i] = turn(a.rot, a.positions[t0 + t], i - t * a.rot.pairs);
+    }
+    __syncthreads();
+    const int lanes = a.d >> 4, per_token = a.H * lanes;
+    for (int i = threadIdx.x; i < n * per_token; i += kThreads) {
+        const int t = i / per_token, in_token = i - t * per_token, h = in_token / lanes, j = in_token - h * lanes;
+        const Pieces p = pieces_of(a.rot, j);
+        const int64_t from = (t0 + t) * a.x_stride + h * a.d, to = (t0 + t) * a.out_stride + h * a.d;
+        const Raw<BF16> r1 = load8<BF16>(a.x, from + 8 * p.first), r2 = load8<BF16>(a.x, from + 8 * p.second);
+        float v[8], w[8];
+        widen8<BF16>(r1, v);
+        widen8<BF16>(r2, w);
+        rotate16(a.rot, turns + t * a.rot.pairs, j, v, w);
+        store8<BF16OUT>(a.out, to + 8 * p.first, v);
+        store8<BF16OUT>(a.out, to + 8 * p.second, w);
+    }
+}
+
+// --- keys and values into the cache ----------------------------------------------------------------------------
+
+struct AppendArgs {
+    const void *k, *v, *q;
+    void* q_out;
+    int64_t k_stride, v_stride, q_stride, q_out_stride;   // values between two tokens
+    PagedCache cache;
+    PagedBatch batch;
+    Rotation rot;
+    int T, Hq, d;
+    float eps;
+};
+
+// The sequence that token t belongs to: the last one that starts at or before it.  (A wave reads 64 starts at once: a search by halves
+// would be a chain of dependent loads.)
+__device__ __forceinline__ int sequence_of(const PagedBatch& b, int t) {
+    int n = 0;
+    for (int s0 = 0; s0 < b.n_seqs; s0 += 64) {
+        const int s = s0 + (threadIdx.x & 63);
+        n += __popcll(__ballot(s < b.n_seqs && b.q_starts[s] <= t));
+    }
+    return n - 1;
+}
+
+template <int BITS>
+__device__ __forceinline__ void store_state(const PagedCache& c, bool keys, int64_t row, int d, const Pieces& p, int lanes, int j,
+                                            float* a, float* b, float eps) {
+    uint8_t* pool = keys ? c.k : c.v;
+    if constexpr (BITS == 16) {
+        if (row >= 0) {
+            store8<true>(pool, row * d + 8 * p.first, a);
+            store8<true>(pool, row * d + 8 * p.second, b);
+        }
+    } else {
+        float gamma = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) gamma = fmaxf(gamma, fmaxf(fabsf(a[i]), fabsf(b[i])));
+        for (int m = 1; m < lanes; m <<= 1) gamma = fmaxf(gamma, __shfl_xor(gamma, m, 64));
+        const float gain = kv_gain<BITS>(gamma, eps);
+        if (row < 0) return;
+        if (j == 0) (keys ? c.k_scales : c.v_scales)[row] = kv_scale<BITS>(gamma);
+        uint32_t u[8], w[8];
+        kv_codes8<BITS>(a, gain, u);
+        kv_codes8<BITS>(b, gain, w);
+        uint8_t* to = pool + row * (d * BITS / 8);
+        if constexpr (BITS == 8) {
+            reinterpret_cast<uint2*>(to)[p.first] = make_uint2(u[0] | (u[1] << 8) | (u[2] << 16) | (u[3] << 24),
+                                                               u[4] | (u[5] << 8) | (u[6] << 16) | (u[7] << 24));
+            reinterpret_cast<uint2*>(to)[p.second] = make_uint2(w[0] | (w[1] << 8) | (w[2] << 16) | (w[3] << 24),
+                                                                w[4] | (w[5] << 8) | (w[6] << 16) | (w[7] << 24));
+        } else {
+            uint32_t x = 0, y = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x |= u[i] << (BITS * i);
+                y |= w[i] << (BITS * i);
+            }
+            if constexpr (BITS == 4) {
+                reinterpret_cast<uint32_t*>(to)[p.first] = x;
+                reinterpret_cast<uint32_t*>(to)[p.second] = y;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 3; ++i) {
+                    to[3 * p.first + i] = (uint8_t)(x >> (8 * i));
+                    to[3 * p.second + i] = (uint8_t)(y >> (8 * i));
+                }
+            }
+        }
+    }
+}
+
+// One token a workgroup row of the grid, its heads (queries, keys, values in this order) over threads and over gridDim.y.
+template <int BITS, bool BF16, bool BF16Q>
+__global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a) {
+    extern __shared__ float2 turns[];   // [pairs]
+    const int t = blockIdx.x;
+    const int s = sequence_of(a.batch, t);
+    if (s < 0) return;   // (before the first sequence, or ...
+    const SeqSpan span = span_of(a.batch, a.cache.page_shift, a.T, s);
+    const int in_seq = t - span.first;
+    if (in_seq >= span.n) return;   // ... behind its end: left as it was)
+    const int position = span.total - span.n + in_seq;
+    for (int i = threadIdx.x; i < a.rot.pairs; i += kThreads) turns[i] = turn(a.rot, position, i);
+    __syncthreads();
+    const int64_t slot = position >= 0 && position < span.keys ? key_row(a.cache, a.batch, s, position, 0) : -1;
+    const int lanes = a.d >> 4, log2_lanes = 31 - __builtin_clz(lanes), heads = a.cache.heads;
+    const int items = (a.Hq + 2 * heads) << log2_lanes;
+    for (int i = (int)blockIdx.y * kThreads + threadIdx.x; i < items; i += (int)gridDim.y * kThreads) {
+        int h = i >> log2_lanes;
+        const int j = i & (lanes - 1);
+        const bool is_q = h < a.Hq, is_k = !is_q && h < a.Hq + heads;
+        h -= is_q ? 0 : (is_k ? a.Hq : a.Hq + heads);
+        const void* x = is_q ? a.q : (is_k ? a.k : a.v);
+        const int64_t from = (int64_t)t * (is_q ? a.q_stride : (is_k ? a.k_stride : a.v_stride)) + h * a.d;
+        Pieces p = pieces_of(a.rot, j);
+        const Raw<BF16> r1 = load8<BF16>(x, from + 8 * p.first), r2 = load8<BF16>(x, from + 8 * p.second);
+        float v[8], w[8];
+        widen8<BF16>(r1, v);
+        widen8<BF16>(r2, w);
+        if (is_q || is_k) rotate16(a.rot, turns, j, v, w);
+        if (is_q) {
+            const int64_t to = (int64_t)t * a.q_out_stride + h * a.d;
+            store8<BF16Q>(a.q_out, to + 8 * p.first, v);
+            store8<BF16Q>(a.q_out, to + 8 * p.second, w);
+        } else {   // (a row's lanes are all of one kind: they take this branch together)
+            store_state<BITS>(a.cache, is_k, slot < 0 ? -1 : slot + ((int64_t)h << a.cache.page_shift), a.d, p, lanes, j, v, w, a.eps);
+        }
+    }
+}
+
+Rotation rotation(const float* freqs, int64_t rot_dim, int layout, float magnitude, bool transposed) {
+    return {freqs, freqs ? (int)(rot_dim / 2) : 0, layout == HBL_ROPE_INTERLEAVED, magnitude, transposed ? -1.0f : 1.0f};
+}
+
+}  // namespace
+
+int launch_rope(const void* x, int x_dtype, int64_t T, int64_t H, int64_t d, int64_t x_stride, const int32_t* positions,
+                const float* freqs, int64_t rot_dim, int layout, float magnitude, bool backward, void* out, int out_dtype,
+                int64_t out_stride, hipStream_t stream) {
+    RopeArgs a{x, out, positions, x_stride, out_stride, (int)T, (int)H, (int)d, 1, rotation(freqs, rot_dim, layout, magnitude, backward)};
+    // short tokens share a workgroup (and its threads compute their factors side by side): enough for a piece each
+    const int64_t per_token = H * (d / 16);
+    while (a.tokens < 16 && a.tokens * 2 * per_token <= kThreads) a.tokens *= 2;
+    const dim3 grid((unsigned)((T + a.tokens - 1) / a.tokens)), block(kThreads);
+    const size_t lds = (size_t)a.tokens * a.rot.pairs * sizeof(float2);   // at most 16 KiB
+    const bool bf = x_dtype == HBL_BF16, bfo = out_dtype == HBL_BF16;
+    auto kern = bf ? (bfo ? rope_kernel<true, true> : rope_kernel<true, false>) : (bfo ? rope_kernel<false, true> : rope_kernel<false, false>);
+    launch_kernel("rope_kernel", kern, grid, block, lds, stream, a);
+    return after_launch();
+}
+
+int launch_kv_append(const PagedCache& cache, int bits, int d, const PagedBatch& batch, const void* k, int64_t k_stride, const void* v,
+                     int64_t v_stride, int x_dtype, int64_t T, const void* q, int64_t Hq, int64_t q_stride, void* q_out, int q_out_dtype,
+                     int64_t q_out_stride, const float* freqs, int64_t rot_dim, int layout, float magnitude, float eps,
+                     hipStream_t stream) {
+    AppendArgs a{k, v, q, q_out, k_stride, v_stride, q_stride, q_out_stride, cache, batch, rotation(freqs, rot_dim, layout, magnitude, false),
+                 (int)T, q ? (int)Hq : 0, d, eps};
+    // few tokens: a token's heads over several workgroups, as long as that fills more of the chip
+    const int64_t items = (int64_t)(a.Hq + 2 * cache.heads) * (d / 16);
+    int64_t parts = 1;
+    while (parts * T < 512 && parts * kThreads < items) parts *= 2;
+    const dim3 grid((unsigned)T, (unsigned)parts), block(kThreads);
+    const size_t lds = (size_t)a.rot.pairs * sizeof(float2);
+    const bool bf = x_dtype == HBL_BF16, bfq = q_out_dtype == HBL_BF16;
+#define HBL_APPEND(B)                                                                                              \
+    launch_kernel("kv_append_kernel", bf ? (bfq ? kv_append_kernel<B, true, true> : kv_append_kernel<B, true, false>)   \
+                                         : (bfq ? kv_append_kernel<B, false, true> : kv_append_kernel<B, false, false>), \
+                  grid, block, lds, stream, a)
+    switch (bits) {
+        case 16: HBL_APPEND(16); break;
+        case 8: HBL_APPEND(8); break;
+        case 4: HBL_APPEND(4); break;
+        default: HBL_APPEND(3); break;
+    }
+#undef HBL_APPEND
+    return after_launch();
+}
+
+}  // namespace hbl

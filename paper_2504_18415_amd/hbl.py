@@ -24,6 +24,8 @@ E_NULL, E_SHAPE, E_BITS, E_DTYPE, E_WORKSPACE, E_HIP, E_ALIGN, E_SCRATCH = -1, -
 F32, BF16 = 0, 1
 CODES_INT8, CODES_UINT4_PLUS8, CODES_BF6 = 0, 8, 6
 EPS = 1e-5
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
 
 EXPORTS = [
     "hbl_strerror", "hbl_last_hip_error", "hbl_ternarize_workspace_bytes", "hbl_ternarize_weights_absmean",
@@ -33,9 +35,11 @@ EXPORTS = [
     "hbl_ln_bitlinear_forward", "hbl_ln_fwht_quant", "hbl_gemm_i32_bf6",
     "hbl_kv_packed_bytes", "hbl_kv_quant_absmax", "hbl_kv_dequant", "hbl_trace_begin", "hbl_trace_end",
     "hbl_code_bytes", "hbl_bitlinear_forward_small",
+    "hbl_rope_frequencies", "hbl_rope", "hbl_kv_append", "hbl_paged_attention_workspace_bytes", "hbl_paged_attention",
 ]
 # exports for the test suite only (csrc/hbl_test_exports.h)
-TEST_EXPORTS = ["hbl_test_grouped_plan", "hbl_test_gemm_i32_tile", "hbl_test_forward_route", "hbl_test_gemm_tile"]
+TEST_EXPORTS = ["hbl_test_grouped_plan", "hbl_test_gemm_i32_tile", "hbl_test_forward_route", "hbl_test_gemm_tile",
+                "hbl_test_kv_rows", "hbl_test_visible_keys"]
 ROUTES = ("fused", "stream", "mid", "prefill", "fused_bytes")
 TILE_SQUARE, TILE_SMALL, TILE_WIDE, TILE_MID, TILE_FEW_TOKENS = 0, 1, 2, 3, 4
 TILE_HALF, TILE_SMALL_FLAT, TILE_NARROW, TILE_NARROW_DEEP = 10, 11, 12, 13
@@ -51,6 +55,19 @@ class Problem(ctypes.Structure):
                 ("K", ctypes.c_int64), ("N", ctypes.c_int64), ("Wq_packed", ctypes.c_void_p),
                 ("w_scales", ctypes.c_void_p), ("n_scale_groups", ctypes.c_int64), ("y", ctypes.c_void_p),
                 ("ln_gain", ctypes.c_void_p), ("ln_eps", ctypes.c_float)]
+
+
+class _Cache(ctypes.Structure):
+    """``hbl_kv_cache`` of include/hbitlinear.h."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int64), ("page_rows", ctypes.c_int64), ("bits", ctypes.c_int), ("page_size", ctypes.c_int),
+                ("n_kv_heads", ctypes.c_int), ("d", ctypes.c_int)]
+
+
+class _Batch(ctypes.Structure):
+    """``hbl_kv_batch`` of include/hbitlinear.h."""
+    _fields_ = [("q_starts", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64), ("n_seqs", ctypes.c_int), ("table_width", ctypes.c_int)]
 
 
 class HblError(RuntimeError):
@@ -111,6 +128,15 @@ def lib():
         L.hbl_grouped_workspace_bytes.restype = sz
         L.hbl_grouped_workspace_bytes.argtypes = [ctypes.POINTER(Problem), ci]
         L.hbl_bitlinear_forward_grouped.argtypes = [ctypes.POINTER(Problem), ci, f32, vp, sz, vp]
+        dbl, cp, bp = ctypes.c_double, ctypes.POINTER(_Cache), ctypes.POINTER(_Batch)
+        L.hbl_rope_frequencies.argtypes = [i64, dbl, ci, dbl, dbl, dbl, dbl, vp]
+        L.hbl_rope.argtypes = [vp, ci, i64, i64, i64, i64, vp, vp, i64, ci, f32, ci, vp, ci, i64, vp]
+        L.hbl_kv_append.argtypes = [cp, bp, vp, i64, vp, i64, ci, i64, vp, i64, i64, vp, ci, i64, vp, i64, ci, f32, f32, vp]
+        L.hbl_paged_attention_workspace_bytes.restype = sz
+        L.hbl_paged_attention_workspace_bytes.argtypes = [cp, bp, i64, i64, i64]
+        L.hbl_paged_attention.argtypes = [vp, i64, i64, i64, cp, bp, i64, f32, f32, i64, vp, vp, vp, i64, vp, sz, vp]
+        L.hbl_test_kv_rows.argtypes = [cp, bp, i64, ci, ctypes.POINTER(i64), ci, ip]
+        L.hbl_test_visible_keys.argtypes = [ci, ci, ci, ci, ip, ip]
         _bind_native(L)
         _lib = L
     return _lib
@@ -576,4 +602,199 @@ def kv_dequant(packed: torch.Tensor, scales: torch.Tensor, d: int, bits: int, ou
     _check_bytes(out, "out", rows * d * (2 if out.dtype == torch.bfloat16 else 4))   # (any other type takes fp32)
     _check(lib().hbl_kv_dequant(_ptr(packed), _ptr(scales), rows, d, bits, _ptr(out),
                                 BF16 if out.dtype == torch.bfloat16 else F32, _stream()), "kv_dequant")
+    return out
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, trained_len: float = 0.0,
+                     slow: float = 1.0, fast: float = 4.0, device="cuda") -> torch.Tensor:
+    """Angles per position of the rot_dim/2 pairs of :func:`rope` (fp32), for contexts beyond the trained one too: ``scaling``
+    is "plain", "linear", "base" or "parts" (the formulas stand with HBL_ROPE_* in include/hbitlinear.h)."""
+    f = torch.empty(max(rot_dim // 2, 0), dtype=torch.float32)
+    _check(lib().hbl_rope_frequencies(rot_dim, base, _choice(ROPE_SCALINGS, "scaling", scaling), factor, trained_len, slow, fast,
+                                      f.data_ptr()), "rope_frequencies")
+    return f.to(device)
+
+
+def _choice(known, what, name):
+    if name not in known:
+        raise ValueError(f"{what} must be one of {', '.join(known)} (got {name!r})")
+    return known[name]
+
+
+def _heads(x: torch.Tensor, what: str):
+    """Head states [T, H, d]: heads contiguous, tokens as far apart as the strides say.  -> (T, H, d, token stride)"""
+    if not x.is_cuda or x.dim() != 3:
+        raise ValueError(f"{what} must be a device tensor [T, H, d]")
+    if x.device.index != (torch.cuda.current_device() if _device_index is None else _device_index()):
+        raise ValueError(f"{what} is on {x.device}, which is not the current device")
+    T, H, d = x.shape
+    st, sh, sd = x.stride()
+    if (sd != 1 and d > 1) or (sh != d and H > 1) or (st < H * d and T > 1):
+        raise ValueError(f"{what} must have contiguous heads, a token's one after the other (got strides {tuple(x.stride())})")
+    return T, H, d, (st if T > 1 else H * d)
+
+
+def _heads_out(out, like, dtype, what: str):
+    """``out`` for head states shaped as ``like``: given, or allocated.  -> (out, token stride)"""
+    if out is None:
+        T, H, d = like.shape
+        return torch.empty((T, H, d), dtype=dtype, device=like.device), H * d
+    if out.shape != like.shape or out.device != like.device:
+        raise ValueError(f"{what} must be {tuple(like.shape)} on {like.device} (got {tuple(out.shape)} on {out.device})")
+    return out, _heads(out, what)[3]
+
+
+def _index(t: torch.Tensor, what: str, numel: int, device):
+    if t.dtype != torch.int32 or t.device != device or not t.is_contiguous() or t.numel() != numel:
+        raise ValueError(f"{what} must be a contiguous int32 tensor of {numel} on {device} (got {t.dtype}, {t.numel()}, {t.device})")
+
+
+def _floats(t: torch.Tensor, what: str, numel: int, device):
+    if t.dtype != torch.float32 or t.device != device or not t.is_contiguous() or t.numel() != numel:
+        raise ValueError(f"{what} must be a contiguous float32 tensor of {numel} on {device} (got {t.dtype}, {t.numel()}, {t.device})")
+
+
+def rope(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, layout: str = "half", magnitude: float = 1.0,
+         backward: bool = False, out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rotary positions of head states x [T, H, d] (a slice of a fused QKV output is taken where it is): the first
+    2 * len(freqs) features of every head turn by positions[t] * freqs[i].  ``backward``: the transposed map, from dL/dy to
+    dL/dx.  ``out`` may be ``x`` itself."""
+    T, H, d, stride = _heads(x, "x")
+    _index(positions, "positions", T, x.device)
+    _floats(freqs, "freqs", freqs.numel(), x.device)
+    out, out_stride = _heads_out(out, x, out_dtype or x.dtype, "out")
+    _check(lib().hbl_rope(_ptr(x), _x_dtype(x), T, H, d, stride, _ptr(positions), _ptr(freqs), 2 * freqs.numel(),
+                          _choice(ROPE_LAYOUTS, "layout", layout), magnitude, int(bool(backward)), _ptr(out), _x_dtype(out),
+                          out_stride, _stream()), "rope")
+    return out
+
+
+class KvCache:
+    """A paged cache of head states (``hbl_kv_cache``): pools k and v of [pages, heads, page size, d] in bf16 (``bits`` 16), or
+    of [pages, heads, page size, d * bits / 8] bytes of codes with fp32 scales [pages, heads, page size].  The pages of a pool
+    may lie apart (one pool for both sides, or for all layers): the stride of the first dimension is free, the same number of
+    rows for all of the cache's tensors.  Holds the tensors and nothing else."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, bits: int = 16, k_scales: Optional[torch.Tensor] = None,
+                 v_scales: Optional[torch.Tensor] = None):
+        if bits not in (16, 8, 4, 3):
+            raise ValueError(f"bits must be 16, 8, 4 or 3 (got {bits})")
+        want = torch.bfloat16 if bits == 16 else torch.uint8
+        if k.dim() != 4 or k.dtype != want or not k.is_cuda:
+            raise ValueError(f"k must be a device tensor of {want} [pages, heads, page size, {'d' if bits == 16 else 'd * bits / 8'}]")
+        n_pages, heads, page, width = k.shape
+        d = width if bits == 16 else width * 8 // bits
+        if bits != 16 and d * bits != width * 8:
+            raise ValueError(f"rows of {width} bytes are no whole number of {bits}-bit codes")
+        if (k_scales is None or v_scales is None) != (bits == 16) or (bits == 16 and (k_scales is not None or v_scales is not None)):
+            raise ValueError("k_scales and v_scales go with codes, and with codes only")
+        page_rows = max(k.stride(0) // max(width, 1), heads * page) if n_pages > 1 else heads * page
+        for name, t, row, dtype in (("k", k, width, want), ("v", v, width, want), ("k_scales", k_scales, 1, torch.float32),
+                                    ("v_scales", v_scales, 1, torch.float32)):
+            if t is None:
+                continue
+            shape = (n_pages, heads, page) + ((width,) if t.dim() == 4 else ())
+            inner = t.dim() == (4 if name in ("k", "v") else 3) and n_pages > 0 and t[0].is_contiguous()
+            if (t.dtype != dtype or t.device != k.device or tuple(t.shape) != shape or not (inner or n_pages == 0)
+                    or (n_pages > 1 and t.stride(0) != page_rows * row)):
+                raise ValueError(f"{name} does not fit k: {dtype} {shape} with pages {page_rows} rows apart on {k.device} "
+                                 f"(got {t.dtype} {tuple(t.shape)}, strides {tuple(t.stride())}, {t.device})")
+        self.k, self.v, self.bits, self.k_scales, self.v_scales = k, v, bits, k_scales, v_scales
+        self.n_pages, self.n_kv_heads, self.page_size, self.d = n_pages, heads, page, d
+        self._c = _Cache(_ptr(k), _ptr(v), _ptr(k_scales), _ptr(v_scales), n_pages, page_rows, bits, page, heads, d)
+        self._ref = ctypes.byref(self._c)
+
+    @classmethod
+    def empty(cls, n_pages: int, n_kv_heads: int, page_size: int, d: int, bits: int = 16, device="cuda") -> "KvCache":
+        """A cache with memory of its own (not cleared: a slot is read only after it is written)."""
+        if bits == 16:
+            k, v = (torch.empty((n_pages, n_kv_heads, page_size, d), dtype=torch.bfloat16, device=device) for _ in range(2))
+            return cls(k, v)
+        k, v = (torch.empty((n_pages, n_kv_heads, page_size, d * bits // 8), dtype=torch.uint8, device=device) for _ in range(2))
+        ks, vs = (torch.empty((n_pages, n_kv_heads, page_size), dtype=torch.float32, device=device) for _ in range(2))
+        return cls(k, v, bits, ks, vs)
+
+
+def _batch(cache: KvCache, q_starts, kv_lens, block_table) -> _Batch:
+    device = cache.k.device
+    n = kv_lens.numel()
+    _index(q_starts, "q_starts", n + 1, device)
+    _index(kv_lens, "kv_lens", n, device)
+    if (block_table.dtype != torch.int32 or block_table.device != device or block_table.dim() != 2 or block_table.shape[0] != n
+            or (block_table.shape[1] > 1 and block_table.stride(1) != 1) or (n > 1 and block_table.stride(0) < block_table.shape[1])):
+        raise ValueError(f"block_table must be int32 [{n}, pages] on {device}, rows contiguous (got {block_table.dtype} "
+                         f"{tuple(block_table.shape)}, strides {tuple(block_table.stride())}, {block_table.device})")
+    width = block_table.shape[1]
+    return _Batch(_ptr(q_starts), _ptr(kv_lens), _ptr(block_table), block_table.stride(0) if n > 1 else width, n, width)
+
+
+def kv_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, q_starts: torch.Tensor, kv_lens: torch.Tensor,
+              block_table: torch.Tensor, freqs: Optional[torch.Tensor] = None, layout: str = "half", magnitude: float = 1.0,
+              q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, eps: float = EPS) -> Optional[torch.Tensor]:
+    """The new tokens' keys and values k, v [T, heads, d] into the cache, the keys rotated to their positions on the way
+    (``freqs`` None: not), quantised as by :func:`kv_quant_absmax` where the cache holds codes.  With ``q`` [T, query heads, d]
+    the queries are rotated by the same launch and returned (in ``q_out`` where given, which may be ``q``).
+
+    The batch: sequence s has the tokens [q_starts[s], q_starts[s+1]), the last ones of its kv_lens[s] keys (these included);
+    its key j lies in page block_table[s][j // page size].  All int32 on the device, read by the kernel."""
+    T, H, d, k_stride = _heads(k, "k")
+    if H != cache.n_kv_heads or d != cache.d or k.device != cache.k.device:
+        raise ValueError(f"k must be [T, {cache.n_kv_heads}, {cache.d}] on {cache.k.device} (got {tuple(k.shape)} on {k.device})")
+    if v.shape != k.shape or v.dtype != k.dtype or v.device != k.device:
+        raise ValueError(f"v must be like k (got {v.dtype} {tuple(v.shape)} on {v.device})")
+    v_stride = _heads(v, "v")[3]
+    Hq = q_stride = q_out_stride = 0
+    if q is not None:
+        if q.dim() != 3 or q.shape[0] != T or q.shape[2] != d or q.dtype != k.dtype or q.device != k.device:
+            raise ValueError(f"q must be {k.dtype} [{T}, query heads, {d}] on {k.device} (got {q.dtype} {tuple(q.shape)} on {q.device})")
+        Hq, q_stride = q.shape[1], _heads(q, "q")[3]
+        q_out, q_out_stride = _heads_out(q_out, q, q.dtype, "q_out")
+    elif q_out is not None:
+        raise ValueError("q_out goes with q")
+    rot = 0
+    if freqs is not None:
+        _floats(freqs, "freqs", freqs.numel(), k.device)
+        rot = 2 * freqs.numel()
+    batch = _batch(cache, q_starts, kv_lens, block_table)
+    _check(lib().hbl_kv_append(cache._ref, ctypes.byref(batch), _ptr(k), k_stride, _ptr(v), v_stride, _x_dtype(k), T, _ptr(q), Hq, q_stride,
+                               _ptr(q_out), BF16 if q is None else _x_dtype(q_out), q_out_stride, _ptr(freqs), rot,
+                               _choice(ROPE_LAYOUTS, "layout", layout), magnitude, eps, _stream()), "kv_append")
+    return q_out
+
+
+def paged_attention_workspace_bytes(cache: KvCache, T: int, n_seqs: int, n_q_heads: int, max_q_len: int) -> int:
+    batch = _Batch(None, None, None, 0, n_seqs, 0)
+    return int(lib().hbl_paged_attention_workspace_bytes(cache._ref, ctypes.byref(batch), T, n_q_heads, max_q_len))
+
+
+def paged_attention(q: torch.Tensor, cache: KvCache, q_starts: torch.Tensor, kv_lens: torch.Tensor, block_table: torch.Tensor,
+                    max_q_len: int, scale: Optional[float] = None, softcap: float = 0.0, window: int = 0,
+                    slopes: Optional[torch.Tensor] = None, prefix_lens: Optional[torch.Tensor] = None,
+                    out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the new tokens' queries q [T, query heads, d] bf16 against the cache, their own keys included: bf16 like q.
+    The batch as for :func:`kv_append`; ``max_q_len`` is at least the new tokens of any sequence; ``scale`` is 1/sqrt(d) where
+    not given.  ``softcap``: scores capped by a tanh; ``window``: keys so far back only; ``slopes`` [query heads] fp32: a bias by
+    distance; ``prefix_lens`` [sequences] int32: the keys that every token sees.  A token that sees nothing gets zeros."""
+    T, Hq, d, q_stride = _heads(q, "q")
+    if q.dtype != torch.bfloat16:
+        raise TypeError("q must be torch.bfloat16")
+    if d != cache.d or q.device != cache.k.device:
+        raise ValueError(f"q must be [T, query heads, {cache.d}] on {cache.k.device} (got {tuple(q.shape)} on {q.device})")
+    batch = _batch(cache, q_starts, kv_lens, block_table)
+    if slopes is not None:
+        _floats(slopes, "slopes", Hq, q.device)
+    if prefix_lens is not None:
+        _index(prefix_lens, "prefix_lens", batch.n_seqs, q.device)
+    if out is not None and out.dtype != torch.bfloat16:
+        raise TypeError("out must be torch.bfloat16")
+    out, out_stride = _heads_out(out, q, torch.bfloat16, "out")
+    L = lib()
+    if workspace is None:
+        n = int(L.hbl_paged_attention_workspace_bytes(cache._ref, ctypes.byref(batch), T, Hq, max_q_len))
+        workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
+    elif workspace.dtype != torch.uint8 or workspace.device != q.device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 device tensor")
+    _check(L.hbl_paged_attention(_ptr(q), T, Hq, q_stride, cache._ref, ctypes.byref(batch), max_q_len,
+                                 d ** -0.5 if scale is None else scale, softcap, window, _ptr(slopes), _ptr(prefix_lens), _ptr(out),
+                                 out_stride, _ptr(workspace), workspace.numel(), _stream()), "paged_attention")
     return out

@@ -1,0 +1,448 @@
+"""GPU tests of rotary positions, the paged cache's append and paged attention, against their definitions in 64 bits
+(paged_reference.py), through the Python binding."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paged_reference as R
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def hbl():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2504_18415_amd import hbl as H
+    H.lib()
+    return H
+
+
+def note(text):
+    print("[gpu-case] " + text, flush=True)
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+# --- rotary positions -------------------------------------------------------------------------------------------
+
+ROPE = [  # T, H, d, rot, extra stride
+    (1, 1, 64, 64, 0), (1, 32, 128, 128, 0), (7, 3, 80, 32, 16), (33, 8, 128, 64, 128), (5, 12, 16, 16, 0), (130, 2, 256, 256, 0),
+    (3, 5, 512, 512, 0), (257, 1, 16, 16, 0), (64, 7, 96, 48, 8 * 96), (1000, 4, 64, 32, 0), (18, 1, 512, 16, 0)]
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("dtype,out_dtype", [(torch.bfloat16, torch.bfloat16), (torch.float32, torch.float32),
+                                             (torch.bfloat16, torch.float32), (torch.float32, torch.bfloat16)])
+@pytest.mark.parametrize("T,H,d,rot,extra", ROPE)
+def test_rope(hbl, T, H, d, rot, extra, dtype, out_dtype, layout):
+    note(f"rope T={T} H={H} d={d} rot={rot} extra={extra} {dtype}->{out_dtype} {layout}")
+    g = gen(T * 131 + d)
+    rows = torch.randn((T, H * d + extra), generator=g).to(dtype).cuda()
+    x = rows[:, extra // 2:extra // 2 + H * d].unflatten(-1, (H, d))
+    positions = torch.randint(0, 1 << 20, (T,), generator=g).to(torch.int32).cuda()
+    positions[0] = 0
+    positions[-1] = -12345 if T > 2 else 2 ** 31 - 1
+    freqs = R.frequencies(rot).cuda()
+    for backward in (False, True):
+        m = 1.25 if backward else 1.0
+        y = hbl.rope(x, positions, freqs, layout=layout, magnitude=m, backward=backward, out_dtype=out_dtype)
+        want = R.rotate(x, positions, freqs, layout, m, backward)
+        tol = R.rotate_bound(x, freqs, layout, m) + (want.abs() * R.U16 * 1.001 if out_dtype == torch.bfloat16 else 0.0)
+        assert y.dtype == out_dtype and ((y.double() - want).abs() <= tol).all()
+        if T > 2:
+            assert torch.equal(y[0, :, rot:].float(), x[0, :, rot:].to(out_dtype).float())
+
+
+def test_rope_in_place_in_a_fused_output(hbl):
+    """Queries and keys turned where the projection left them; values and what lies beside untouched."""
+    note("rope in place")
+    T, H, d = 37, 4, 64
+    qkv = torch.randn((T, 3 * H * d), generator=gen(3)).bfloat16().cuda()
+    before, positions, freqs = qkv.clone(), torch.arange(T, dtype=torch.int32, device="cuda") + 100, R.frequencies(d).cuda()
+    for part in (0, 1):
+        x = qkv[:, part * H * d:(part + 1) * H * d].unflatten(-1, (H, d))
+        assert hbl.rope(x, positions, freqs, out=x).data_ptr() == x.data_ptr()
+    want = hbl.rope(before[:, :2 * H * d].unflatten(-1, (2 * H, d)), positions, freqs)
+    assert torch.equal(qkv[:, :2 * H * d].view(torch.int16), want.flatten(1).view(torch.int16))
+    assert torch.equal(qkv[:, 2 * H * d:], before[:, 2 * H * d:])
+
+
+def test_rope_backward_is_the_gradient(hbl):
+    """<rope(x), g> and <x, backward(g)> agree, and differences of the forward map give the same."""
+    note("rope gradient")
+    T, H, d, rot = 9, 2, 64, 32
+    g0 = gen(11)
+    x, g = (torch.randn((T, H, d), generator=g0).cuda() for _ in range(2))
+    positions, freqs = torch.arange(T, dtype=torch.int32, device="cuda") * 1001, R.frequencies(rot).cuda()
+    for layout in ("half", "interleaved"):
+        y = hbl.rope(x, positions, freqs, layout=layout, magnitude=0.75)
+        dx = hbl.rope(g, positions, freqs, layout=layout, magnitude=0.75, backward=True)
+        a, b = (y.double() * g.double()).sum(), (x.double() * dx.double()).sum()
+        slack = (R.rotate_bound(x, freqs, layout, 0.75) * g.abs()).sum() + (R.rotate_bound(g, freqs, layout, 0.75) * x.abs()).sum()
+        assert (a - b).abs() <= slack
+        step = torch.zeros_like(x)
+        step[4, 1, 3] = 1.0   # the map is linear: one step gives a column of it
+        column = hbl.rope(step, positions, freqs, layout=layout, magnitude=0.75)
+        tol = (R.rotate_bound(step, freqs, layout, 0.75) * g.abs()).sum() + R.rotate_bound(g, freqs, layout, 0.75)[4, 1, 3]
+        assert ((column.double() * g.double()).sum() - dx[4, 1, 3].double()).abs() <= tol
+
+
+# --- append -----------------------------------------------------------------------------------------------------
+
+APPEND = [  # new tokens, lengths, Hq, Hkv, page
+    ([1], [1], 1, 1, 16), ([1, 1, 1], [5, 64, 65], 8, 2, 16), ([130], [130], 4, 4, 64), ([0, 7, 0, 33, 1], [9, 7, 0, 100, 3], 6, 2, 32),
+    ([1] * 70, list(range(1, 71)), 2, 1, 16), ([5, 4], [3, 4], 3, 3, 128)]   # (the last: two tokens before the first position)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("bits", [16, 8, 4, 3])
+@pytest.mark.parametrize("d,rot", [(64, 32), (128, 128), (256, 64)])
+@pytest.mark.parametrize("case", range(len(APPEND)))
+def test_append(hbl, case, d, rot, bits, dtype, layout):
+    new, lens, Hq, Hkv, page = APPEND[case]
+    note(f"append case={case} d={d} rot={rot} bits={bits} {dtype} {layout}")
+    g = gen(case * 7 + bits)
+    T = sum(new) + 2   # two tokens behind the last sequence
+    qkv = torch.randn((T, (Hq + 2 * Hkv) * d), generator=g).to(dtype).cuda()
+    q, k, v = (p.unflatten(-1, (-1, d)) for p in qkv.split((Hq * d, Hkv * d, Hkv * d), -1))
+    table, n_pages = R.page_table(g, lens, page, spare=2)
+    (kp, ks), (vp, vs) = (R.random_pages(g, n_pages, Hkv, page, d, bits, "cuda") for _ in range(2))
+    was = [None if t is None else t.clone() for t in (kp, vp, ks, vs)]
+    cache = hbl.KvCache(kp, vp, bits, ks, vs)
+    starts = [0]
+    for n in new:
+        starts.append(starts[-1] + n)
+    freqs = R.frequencies(rot).cuda()
+    q_out = torch.full((T, Hq, d), 7.0, dtype=dtype, device="cuda")
+    got = hbl.kv_append(cache, k, v, ints(starts), ints(lens), table.cuda(), freqs=freqs, layout=layout, q=q, q_out=q_out)
+    assert got is q_out
+    torch.cuda.synchronize()
+    position = torch.zeros(T, dtype=torch.int32)
+    where = []
+    for s, n in enumerate(new):
+        for i in range(n):
+            p = lens[s] - n + i
+            position[starts[s] + i] = p
+            if p >= 0:
+                where.append((starts[s] + i, int(table[s, p // page]), p % page))
+    # what rope and kv_quant_absmax give, bit for bit
+    live = starts[-1]
+    k32 = hbl.rope(k, position.cuda(), freqs, layout=layout, out_dtype=torch.float32)
+    want_q = hbl.rope(q, position.cuda(), freqs, layout=layout)
+    assert torch.equal(q_out[:live], want_q[:live]) and (q_out[live:] == 7.0).all()
+    want = [None if t is None else t.clone() for t in was]
+    for side, x in ((0, k32), (1, v.float())):
+        if bits == 16:
+            rows, scales = x.bfloat16(), None
+        else:
+            rows, scales = hbl.kv_quant_absmax(x.contiguous().view(T * Hkv, d), bits)
+            rows, scales = rows.view(T, Hkv, -1), scales.view(T, Hkv)
+        for t, p, slot in where:
+            want[side][p, :, slot] = rows[t]
+            if bits != 16:
+                want[2 + side][p, :, slot] = scales[t]
+    for a, b in zip((kp, vp, ks, vs), want):   # every other row as it was
+        assert a is None or torch.equal(a.view(torch.int16) if a.dtype == torch.bfloat16 else a, b.view(torch.int16) if b.dtype == torch.bfloat16 else b)
+
+
+def test_append_without_rotation_queries_or_pages(hbl):
+    note("append: no rotation, entries that name no page, a table that ends early, an interleaved pool")
+    d, page, H = 64, 16, 2
+    pool = torch.zeros((6, 2, H, page, d), dtype=torch.bfloat16, device="cuda")   # keys and values side by side
+    cache = hbl.KvCache(pool[:, 0], pool[:, 1])
+    k, v = (torch.randn((60, H, d), generator=gen(5)).bfloat16().cuda() for _ in range(2))
+    table = ints([[3, -1, 6, 0], [2 ** 31 - 1, 4, 1, 5]])[:, :3]
+    # sequence 0: 30 tokens at 20..49: slots 4.. of no page, of a page that is not there (6), beyond the table's three pages
+    assert hbl.kv_append(cache, k, v, ints([0, 30, 60]), ints([50, 47]), table) is None
+    torch.cuda.synchronize()
+    want = torch.zeros_like(pool)
+    for i in range(30):   # sequence 1: tokens at 17..46
+        p = 17 + i
+        if p // page < 3 and [None, 4, 1][p // page] is not None:
+            want[[None, 4, 1][p // page], 0, :, p % page], want[[None, 4, 1][p // page], 1, :, p % page] = k[30 + i], v[30 + i]
+    assert torch.equal(pool, want)
+
+
+# --- attention --------------------------------------------------------------------------------------------------
+
+def check_attention(hbl, new, lens, Hq, Hkv, d, bits, page, seed=0, tail=0, pad_table=0, table_edit=None, q_scale=2.0, max_q_len=None,
+                    **options):
+    g = gen(seed + 1000 * bits + d)
+    T = sum(new) + tail
+    table, n_pages = R.page_table(g, lens, page, spare=1, width=pad_table)
+    if table_edit is not None:
+        table_edit(table)
+    (kp, ks), (vp, vs) = (R.random_pages(g, n_pages, Hkv, page, d, bits, "cuda") for _ in range(2))
+    vp = vp if bits != 16 else (vp.float() + 0.5).bfloat16()
+    # fused layout: the queries are a slice of wider rows
+    q = (q_scale * torch.randn((T, (Hq + 2) * d), generator=g)).bfloat16().cuda()[:, d:-d].unflatten(-1, (Hq, d))
+    starts = [0]
+    for n in new:
+        starts.append(starts[-1] + n)
+    slopes, prefix = options.get("slopes"), options.get("prefix_lens")
+    cache = hbl.KvCache(kp, vp, bits, ks, vs)
+    out = torch.full((T, Hq, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    kw = {**options, "slopes": None if slopes is None else torch.tensor(slopes, device="cuda"), "prefix_lens": None if prefix is None else ints(prefix)}
+    got = hbl.paged_attention(q, cache, ints(starts), ints(lens), table.cuda(), max_q_len or max(max(new, default=1), 1), out=out, **kw)
+    assert got is out
+    torch.cuda.synchronize()
+    kw["prefix_lens"] = prefix
+    scale = kw.pop("scale", None)
+    want, bound = R.attention(q, kp, vp, ks, vs, bits, starts, lens, table.tolist(), d ** -0.5 if scale is None else scale,
+                              **{k: v for k, v in kw.items() if k in ("softcap", "window", "slopes", "prefix_lens")})
+    live = starts[-1]
+    error = (out[:live].double() - want[:live]).abs()
+    tol = bound[:live] + (want[:live].abs() + bound[:live]) * R.U16 * 1.001
+    assert torch.isfinite(out.float()).all()
+    worst = (error - tol).max() if live else torch.tensor(0.0)
+    assert (error <= tol).all(), f"worst excess {float(worst):.3e}, largest error {float(error.max()):.3e}"
+    assert (out[live:] == 7.0).all()
+    return out
+
+
+DECODE = [  # new, lens, Hq, Hkv, page
+    ([1], [1], 1, 1, 16), ([1], [17], 2, 1, 16), ([1, 1], [33, 1000], 8, 2, 64), ([1] * 5, [1, 15, 16, 31, 32], 4, 4, 16),
+    ([1, 0, 1, 1], [64, 10, 0, 700], 32, 8, 128), ([1], [4097], 7, 1, 32), ([2, 3, 1], [2, 259, 600], 8, 4, 64),
+    ([1, 4], [2500, 4], 16, 2, 256), ([1] * 3, [130, 65, 300], 64, 2, 1024), ([1] * 40, [37 * i + 1 for i in range(40)], 4, 2, 64)]
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4, 3])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("case", range(len(DECODE)))
+def test_attention_decode(hbl, case, d, bits):
+    new, lens, Hq, Hkv, page = DECODE[case]
+    note(f"attention decode case={case} d={d} bits={bits}")
+    check_attention(hbl, new, lens, Hq, Hkv, d, bits, page, seed=case, tail=case % 3)
+
+
+CHUNK = [  # new, lens, Hq, Hkv, page
+    ([33], [33], 2, 2, 16), ([64], [64], 4, 2, 64), ([65, 1], [130, 77], 4, 1, 16), ([200], [1000], 2, 1, 128), ([17, 90, 0, 3], [17, 300, 5, 4], 3, 3, 32),
+    ([257], [300], 5, 1, 64), ([40, 300], [30, 300], 2, 2, 16), ([128], [2100], 8, 8, 256), ([511], [511], 1, 1, 1024)]
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4, 3])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("case", range(len(CHUNK)))
+def test_attention_chunk(hbl, case, d, bits):
+    new, lens, Hq, Hkv, page = CHUNK[case]
+    note(f"attention chunk case={case} d={d} bits={bits}")
+    check_attention(hbl, new, lens, Hq, Hkv, d, bits, page, seed=50 + case, tail=case % 2)
+
+
+OPTIONS = [
+    dict(softcap=30.0), dict(softcap=1.5, scale=0.3), dict(window=1), dict(window=100), dict(slopes=True), dict(prefix_lens=[70, 3, 0]),
+    dict(prefix_lens=[1000, 1000, 2], window=50), dict(softcap=20.0, window=333, slopes=True, prefix_lens=[0, 5, 9]), dict(scale=0.0),
+    dict(scale=-0.05)]
+
+
+@pytest.mark.parametrize("bits,d", [(16, 128), (4, 64), (8, 256), (3, 128)])
+@pytest.mark.parametrize("new,lens", [([1, 1, 1], [500, 1, 77]), ([50, 130, 1], [400, 130, 9])])
+@pytest.mark.parametrize("option", range(len(OPTIONS)))
+def test_attention_options(hbl, option, new, lens, bits, d):
+    note(f"attention option={option} new={new} bits={bits} d={d}")
+    kw = dict(OPTIONS[option])
+    if kw.get("slopes"):
+        kw["slopes"] = [2.0 ** (-i - 1) for i in range(4)]
+    check_attention(hbl, new, lens, 4, 2, d, bits, 32, seed=90 + option, **kw)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("new", [[1, 1, 1], [60, 70, 80]])
+def test_attention_with_pages_that_are_not_there(hbl, new, bits):
+    """Entries that name no page leave their keys out; a row that sees nothing else gets zeros."""
+    note(f"attention: absent pages new={new} bits={bits}")
+
+    def edit(table):
+        table[0, :] = -1                       # nothing at all
+        table[1, 0] = 2 ** 31 - 1
+        table[1, 2] = -2 ** 31
+        table[2, 3:] = 10 ** 6
+
+    check_attention(hbl, new, [100, 300, 200], 4, 2, 128, bits, 32, seed=7, table_edit=edit)
+    check_attention(hbl, new, [100, 300, 200], 4, 2, 128, bits, 32, seed=8, table_edit=edit, window=20)
+
+
+def test_attention_lengths_beyond_the_table(hbl):
+    note("attention: lengths beyond the table")
+    g = gen(4)
+    (kp, _), (vp, _) = (R.random_pages(g, 4, 1, 16, 64, 16, "cuda") for _ in range(2))
+    q = torch.randn((5, 2, 64), generator=g).bfloat16().cuda()
+    table = ints([[0, 1], [2, 3]])
+    starts, lens = [0, 2, 5], [90, 32]
+    out = hbl.paged_attention(q, hbl.KvCache(kp, vp), ints(starts), ints(lens), table, 3)
+    want, bound = R.attention(q, kp, vp, None, None, 16, starts, lens, table.tolist(), 64 ** -0.5)
+    assert ((out.double() - want).abs() <= bound + (want.abs() + bound) * R.U16 * 1.001).all()
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4, 3])
+@pytest.mark.parametrize("new,lens", [([1, 1], [90, 300]), ([70, 40], [90, 300])])
+def test_what_masked_places_hold_does_not_count(hbl, new, lens, bits):
+    """NaN and infinities behind the last key, in pages of nobody and in scales of unused slots leave no trace."""
+    note(f"attention: NaN in masked places new={new} bits={bits}")
+    d, page, H = 128, 64, 2
+    g = gen(12)
+    table, n_pages = R.page_table(g, lens, page, spare=2)
+    (kp, ks), (vp, vs) = (R.random_pages(g, n_pages, H, page, d, bits, "cuda") for _ in range(2))
+    q = torch.randn((sum(new), 4, d), generator=g).bfloat16().cuda()
+    starts = ints([0, new[0], sum(new)])
+    args = (starts, ints(lens), table.cuda(), max(new))
+    clean = hbl.paged_attention(q, hbl.KvCache(kp, vp, bits, ks, vs), *args)
+    used = torch.zeros((n_pages, page), dtype=torch.bool)
+    for s, n in enumerate(lens):
+        for j in range(n):
+            used[int(table[s, j // page]), j % page] = True
+    for t in (kp, vp, ks, vs):
+        if t is not None and t.dtype != torch.uint8:
+            m = (~used).cuda()[:, None, :].expand(n_pages, H, page)
+            for i, bad in enumerate((float("nan"), float("inf"), -float("inf"))):
+                pick = m & ((torch.arange(page, device="cuda") % 3) == i)
+                t[pick] = bad
+    dirty = hbl.paged_attention(q, hbl.KvCache(kp, vp, bits, ks, vs), *args)
+    assert torch.equal(clean.view(torch.int16), dirty.view(torch.int16))
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("new", [1, 64])
+def test_attention_of_large_scores(hbl, new, bits):
+    """Scores of thousands: one key takes all, and nothing overflows."""
+    note(f"attention: large scores new={new} bits={bits}")
+    check_attention(hbl, [new, new], [300, 400], 4, 2, 128, bits, 32, seed=3, q_scale=512.0)
+
+
+@pytest.mark.parametrize("bits", [8, 4, 3])
+def test_attention_of_scales_far_apart(hbl, bits):
+    """Rows of zeros (scale 0), tiny and huge scales of values side by side."""
+    note(f"attention: scales far apart bits={bits}")
+    d, page, H = 64, 16, 1
+    g = gen(21)
+    lens, new = [200, 33], [40, 1]
+    table, n_pages = R.page_table(g, lens, page)
+    (kp, ks), (vp, vs) = (R.random_pages(g, n_pages, H, page, d, bits, "cuda") for _ in range(2))
+    vs[:, :, 0::4] = 0.0
+    vs[:, :, 1::4] *= 1e-20
+    vs[:, :, 2::4] *= 1e20
+    ks[:, :, 3::5] = 0.0
+    q = torch.randn((41, 2, d), generator=g).bfloat16().cuda()
+    out = hbl.paged_attention(q, hbl.KvCache(kp, vp, bits, ks, vs), ints([0, 40, 41]), ints(lens), table.cuda(), 40)
+    want, bound = R.attention(q, kp, vp, ks, vs, bits, [0, 40, 41], lens, table.tolist(), d ** -0.5)
+    assert ((out.double() - want).abs() <= bound + (want.abs() + bound) * R.U16 * 1.001).all()
+
+
+def test_attention_same_bits_every_time(hbl):
+    """No result depends on the order in which workgroups finish, nor on what the workspace held."""
+    note("attention: repeated")
+    g = gen(31)
+    lens, new, d, page = [3000, 800, 1], [1, 1, 1], 128, 64
+    table, n_pages = R.page_table(g, lens, page)
+    (kp, _), (vp, _) = (R.random_pages(g, n_pages, 4, page, d, 16, "cuda") for _ in range(2))
+    cache, q = hbl.KvCache(kp, vp), torch.randn((3, 8, d), generator=g).bfloat16().cuda()
+    args = (ints([0, 1, 2, 3]), ints(lens), table.cuda(), 1)
+    n = hbl.paged_attention_workspace_bytes(cache, 3, 3, 8, 1)
+    first = hbl.paged_attention(q, cache, *args)
+    for fill in (0, 255, 127):
+        again = hbl.paged_attention(q, cache, *args, workspace=torch.full((n,), fill, dtype=torch.uint8, device="cuda"))
+        assert torch.equal(first.view(torch.int16), again.view(torch.int16))
+
+
+# --- together ---------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("bits", [16, 8, 4, 3])
+def test_generation_in_steps_equals_one_prompt(hbl, bits):
+    """A prompt in one call, and the same tokens in chunks and single steps over the growing cache: append, attend."""
+    note(f"generation in steps bits={bits}")
+    T, Hq, Hkv, d, page = 150, 8, 2, 128, 16
+    g = gen(41)
+    qkv = torch.randn((T, (Hq + 2 * Hkv) * d), generator=g).bfloat16().cuda()
+    parts = lambda x: [p.unflatten(-1, (-1, d)) for p in x.split((Hq * d, Hkv * d, Hkv * d), -1)]
+    freqs = hbl.rope_frequencies(d, scaling="parts", factor=4.0, trained_len=64.0)
+    table = torch.randperm(10, generator=g).to(torch.int32).cuda().view(1, 10)
+
+    def go(steps):
+        cache, outs, at = hbl.KvCache.empty(10, Hkv, page, d, bits), [], 0
+        for n in steps:
+            q, k, v = parts(qkv[at:at + n])
+            at += n
+            batch = (ints([0, n]), ints([at]), table)
+            q = hbl.kv_append(cache, k, v, *batch, freqs=freqs, q=q)
+            outs.append(hbl.paged_attention(q, cache, *batch, n))
+        return torch.cat(outs), cache
+
+    whole, cache = go([T])
+    steps, other = go([64, 1, 1, 33, 2, 1, 40, 8])
+    assert torch.equal(cache.k[table[0, :9].long()].view(torch.uint8), other.k[table[0, :9].long()].view(torch.uint8))
+    q = hbl.rope(parts(qkv)[0], torch.arange(T, dtype=torch.int32, device="cuda"), freqs)
+    want, bound = R.attention(q, cache.k, cache.v, cache.k_scales, cache.v_scales, bits, [0, T], [T], table.tolist(), d ** -0.5)
+    tol = bound + (want.abs() + bound) * R.U16 * 1.001
+    assert ((whole.double() - want).abs() <= tol).all() and ((steps.double() - want).abs() <= tol).all()
+
+
+def test_decode_steps_in_a_graph(hbl):
+    """A captured step (append and attend) replayed while lengths grow on the device, against eager calls."""
+    note("decode steps in a graph")
+    S, Hq, Hkv, d, page, bits = 3, 8, 4, 64, 16, 4
+    g = gen(51)
+    cache, twin = (hbl.KvCache.empty(S * 8, Hkv, page, d, bits) for _ in range(2))
+    table = torch.randperm(S * 8, generator=g).to(torch.int32).cuda().view(S, 8)
+    freqs, starts = hbl.rope_frequencies(d), ints([0, 1, 2, 3])
+    new = [torch.randn((S, (Hq + 2 * Hkv) * d), generator=g).bfloat16().cuda() for _ in range(40)]
+    hold, lens = new[0].clone(), ints([0, 0, 0])
+    lens_now = ints([0, 0, 0])
+    workspace = torch.empty(hbl.paged_attention_workspace_bytes(cache, S, S, Hq, 1), dtype=torch.uint8, device="cuda")
+
+    def step(x, c, lens, workspace):
+        q, k, v = (p.unflatten(-1, (-1, d)) for p in x.split((Hq * d, Hkv * d, Hkv * d), -1))
+        q = hbl.kv_append(c, k, v, starts, lens, table, freqs=freqs, q=q)
+        return hbl.paged_attention(q, c, starts, lens, table, 1, workspace=workspace)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(hold, cache, lens + 1, workspace)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lens.add_(1)
+        y = step(hold, cache, lens, workspace)
+    lens.zero_()
+    for x in new:
+        hold.copy_(x)
+        graph.replay()
+        lens_now += 1
+        want = step(x, twin, lens_now, None)
+        torch.cuda.synchronize()
+        assert torch.equal(y.view(torch.int16), want.view(torch.int16))
+
+
+def test_two_streams_at_once(hbl):
+    note("two streams")
+    d, page = 128, 64
+    work = []
+    for i, bits in enumerate((16, 4)):
+        g = gen(60 + i)
+        lens = [700 + 100 * i, 50]
+        table, n = R.page_table(g, lens, page)
+        (kp, ks), (vp, vs) = (R.random_pages(g, n, 2, page, d, bits, "cuda") for _ in range(2))
+        q = torch.randn((2, 8, d), generator=g).bfloat16().cuda()
+        work.append((q, hbl.KvCache(kp, vp, bits, ks, vs), ints([0, 1, 2]), ints(lens), table.cuda(), 1))
+    want = [hbl.paged_attention(*w) for w in work]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in work]
+    got = [[], []]
+    for _ in range(20):
+        for i, w in enumerate(work):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(hbl.paged_attention(*w))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for y in got[i]:
+            assert torch.equal(y.view(torch.int16), want[i].view(torch.int16))

@@ -659,7 +659,7 @@ int hbl_kv_append(const hbl_kv_cache* cache, const hbl_kv_batch* batch, const vo
 size_t hbl_paged_attention_workspace_bytes(const hbl_kv_cache* cache, const hbl_kv_batch* batch, int64_t T, int64_t n_q_heads,
                                            int64_t max_q_len) {
     if (check_attention_shape(cache, batch, T, n_q_heads, max_q_len) != HBL_OK) return 0;
-    return paged_attention_workspace(T, batch->n_seqs, (int)n_q_heads, cache->n_kv_heads, cache->d, max_q_len);
+    return paged_attention_workspace(T, batch->n_seqs, (int)n_q_heads, cache->n_kv_heads, cache->d, max_q_len < T ? max_q_len : T);
 }
 
 int hbl_paged_attention(const void* q, int64_t T, int64_t n_q_heads, int64_t q_stride, const hbl_kv_cache* cache,
@@ -675,8 +675,7 @@ int hbl_paged_attention(const void* q, int64_t T, int64_t n_q_heads, int64_t q_s
     if ((rc = check_heads(out, HBL_BF16, T, n_q_heads, cache->d, out_stride)) != HBL_OK) return rc;
     if (!workspace) return HBL_E_NULL;
     if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return HBL_E_ALIGN;
-    if (workspace_bytes < paged_attention_workspace(T, batch->n_seqs, (int)n_q_heads, cache->n_kv_heads, cache->d, max_q_len))
-        return HBL_E_WORKSPACE;
+    if (workspace_bytes < hbl_paged_attention_workspace_bytes(cache, batch, T, n_q_heads, max_q_len)) return HBL_E_WORKSPACE;
     AttentionArgs a{};
     a.q = static_cast<const uint16_t*>(q);
     a.out = static_cast<uint16_t*>(out);
@@ -692,7 +691,8 @@ int hbl_paged_attention(const void* q, int64_t T, int64_t n_q_heads, int64_t q_s
     a.group = (int)(n_q_heads / cache->n_kv_heads);
     a.d = cache->d;
     a.window = (int)window;
-    return launch_paged_attention(a, cache->bits, max_q_len, workspace, static_cast<hipStream_t>(stream));
+    a.max_q = (int)(max_q_len < T ? max_q_len : T);
+    return launch_paged_attention(a, cache->bits, workspace, static_cast<hipStream_t>(stream));
 }
 
 int hbl_test_kv_rows(const hbl_kv_cache* cache, const hbl_kv_batch* batch, int64_t T, int seq, int64_t* rows, int n_rows, int* span) {

@@ -1,9 +1,20 @@
-// What the kernels of paged_attention.hip and its companions take.
+// What the attention kernels share: arguments, the forms in which states reach the matrix cores, and the joining of partial results.
+//
+// Scores are computed transposed, S^T = K Q^T, and so are outputs, O^T = V^T P^T: in either product a column of the result is a row of
+// the softmax (one token and query head), so a lane holds scores of one row only.  Maxima and sums are taken over its registers and
+// over the few lanes of the same column, and the weights P are where the second product wants them, up to the order of the keys, which
+// may be any as long as V is read in the same one.
+//
+// Codes go to the matrix cores as bf16 integers, exactly; scales are applied to scores and weights in fp32.  A code u becomes
+//   3 bits: 8 + u, 4 bits: 16 + u (the code's bits are put into the mantissa: one operation a value), 8 bits: u
+// that is, its value plus a constant `kBias`.  Sums are rid of the constant afterwards: that of the scores starts at -kBias sum(q), that
+// of the outputs ends with -kBias sum(p), both taken over the very numbers that were multiplied.
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "kv_codes.h"
 #include "paged.h"
 
 namespace hbl {
@@ -18,10 +29,113 @@ struct AttentionArgs {
     const int32_t* prefix_lens;   // [n_seqs] or nullptr
     float scale, softcap;
     int T, group, d, window;      // group: query heads of a key head
+    int max_q;                    // tokens of a sequence that are looked at
+    float* partial;               // workspace
 };
 
 // Bytes of workspace of a call (T tokens, n_seqs sequences, Hq / Hkv heads of d).
 size_t paged_attention_workspace(int64_t T, int n_seqs, int Hq, int Hkv, int d, int64_t max_q_len);
-int launch_paged_attention(const AttentionArgs& a, int bits, int64_t max_q_len, void* workspace, hipStream_t stream);
+int launch_paged_attention(const AttentionArgs& a, int bits, void* workspace, hipStream_t stream);
+
+// Few rows a key head (paged_decode.hip): at most kDecodeRows tokens times query heads of a group.
+constexpr int kDecodeRows = 32;
+size_t paged_decode_workspace(int rows, int d);
+int launch_paged_decode(const AttentionArgs& a, int bits, hipStream_t stream);
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {   // round to nearest even
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){lo, hi}, bf16x2));
+}
+
+template <int BITS>
+struct Codes {
+    static constexpr float kBias = BITS == 16 ? 0.0f : BITS == 8 ? 128.0f : BITS == 4 ? 24.0f : 12.0f;
+    // 8 values that come from 8 consecutive features lie in the order kOrder of them (pairs of nibbles four apart share a word)
+    static constexpr bool kPaired = BITS == 4 || BITS == 3;
+};
+// Place, among 8 consecutive features, of the value at position i of the converted order.
+template <int BITS>
+__host__ __device__ constexpr int feature_at(int i) {
+    return Codes<BITS>::kPaired ? (i >> 1) + 4 * (i & 1) : i;
+}
+
+// 8 codes of a row, from the dwords that hold them, as 8 bf16 (value + kBias) in the converted order.  `g`: which eight of the chunk.
+template <int BITS>
+__device__ __forceinline__ u32x4 widen_codes(const uint32_t* w, int g) {
+    if constexpr (BITS == 16) {
+        return (u32x4){w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]};
+    } else if constexpr (BITS == 8) {
+        u32x4 r;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t x = w[2 * g + i];
+            // (the float of an integer below 256 has its upper half's bits only: that half is the bf16)
+            const uint32_t a = as_u((float)(x & 0xFFu)), b = as_u((float)((x >> 8) & 0xFFu)), c = as_u((float)((x >> 16) & 0xFFu)), e = as_u((float)(x >> 24));
+            r[2 * i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+            r[2 * i + 1] = __builtin_amdgcn_perm(e, c, 0x07060302u);
+        }
+        return r;
+    } else if constexpr (BITS == 4) {
+        const uint32_t x = w[g];   // 0x4180 = 16.0, of which a mantissa step is 1/8
+        return (u32x4){((x << 3) & 0x00780078u) | 0x41804180u, ((x >> 1) & 0x00780078u) | 0x41804180u,
+                       ((x >> 5) & 0x00780078u) | 0x41804180u, ((x >> 9) & 0x00780078u) | 0x41804180u};
+    } else {
+        // 24 bits from bit 24 g of the chunk on; codes 4 to 7 are moved up to bit 16
+        const uint32_t lo = w[(3 * g) >> 2];
+        const int at = (3 * g) & 3;
+        const uint32_t x = at == 0 ? lo : at == 1 ? lo >> 8 : __builtin_amdgcn_alignbyte(w[((3 * g) >> 2) + 1], lo, at);
+        const uint32_t y = (x & 0xFFFu) | ((x & 0xFFF000u) << 4);   // 0x4100 = 8.0, of which a mantissa step is 1/16
+        return (u32x4){((y << 4) & 0x00700070u) | 0x41004100u, ((y << 1) & 0x00700070u) | 0x41004100u,
+                       ((y >> 2) & 0x00700070u) | 0x41004100u, ((y >> 5) & 0x00700070u) | 0x41004100u};
+    }
+}
+
+// N dwords from a 4-byte aligned address.
+template <int N>
+__device__ __forceinline__ void load_dwords(const void* p, uint32_t* w) {
+    struct __attribute__((packed, aligned(4))) Chunk {
+        uint32_t w[N];
+    };
+    const Chunk c = *reinterpret_cast<const Chunk*>(p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = c.w[i];
+}
+
+// x op (the value of the lane 32, or 16, away), in every lane.
+template <typename Op>
+__device__ __forceinline__ float join32(float x, Op op) {
+    const auto r = __builtin_amdgcn_permlane32_swap(as_u(x), as_u(x), false, false);
+    return op(as_f(r[0]), as_f(r[1]));
+}
+template <typename Op>
+__device__ __forceinline__ float join16(float x, Op op) {
+    const auto r = __builtin_amdgcn_permlane16_swap(as_u(x), as_u(x), false, false);
+    return op(as_f(r[0]), as_f(r[1]));
+}
+struct MaxOf {
+    __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct SumOf {
+    __device__ float operator()(float a, float b) const { return a + b; }
+};
+
+// The score after cap and bias, in units of log 2.
+__device__ __forceinline__ float shaped_score(float s, float softcap, float slope, int distance) {
+    if (softcap > 0.0f) {
+        // tanh x = 1 - 2 / (e^(2x) + 1): the ends come out right where e^(2x) is 0 or infinite
+        const float e = __builtin_amdgcn_exp2f(s * (2.0f * kLog2e / softcap));
+        s = softcap * (1.0f - 2.0f * __builtin_amdgcn_rcpf(e + 1.0f));
+    }
+    return (s - slope * (float)distance) * kLog2e;
+}
 
 }  // namespace hbl

@@ -84,9 +84,15 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(AttentionArgs a) {
 
 }  // namespace
 
-size_t paged_attention_workspace(int64_t, int, int, int, int, int64_t) { return 256; }
+size_t paged_attention_workspace(int64_t, int, int Hq, int Hkv, int d, int64_t max_q_len) {
+    const int64_t rows = max_q_len * (Hq / Hkv);
+    return rows <= kDecodeRows ? round_up(paged_decode_workspace((int)rows, d), 256) : 256;
+}
 
-int launch_paged_attention(const AttentionArgs& a, int bits, int64_t, void*, hipStream_t stream) {
+int launch_paged_attention(const AttentionArgs& args, int bits, void* workspace, hipStream_t stream) {
+    AttentionArgs a = args;
+    a.partial = static_cast<float*>(workspace);
+    if ((int64_t)a.max_q * a.group <= kDecodeRows) return launch_paged_decode(a, bits, stream);
     const dim3 grid((unsigned)a.T, (unsigned)(a.group * a.cache.heads)), block(256);
     auto kern = bits == 16 ? paged_attention_kernel<16> : bits == 8 ? paged_attention_kernel<8> : bits == 4 ? paged_attention_kernel<4> : paged_attention_kernel<3>;
     launch_kernel("paged_attention_kernel", kern, grid, block, 0, stream, a);

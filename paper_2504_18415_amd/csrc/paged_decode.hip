@@ -1,0 +1,511 @@
+// Attention of few rows (tokens times query heads of a key head, at most 32) against the paged cache: single tokens, speculative batches.
+//
+// Bound by the cache's bytes: every key and value row of a head is read once, for all rows of the group together.  The work is cut
+// evenly whatever the lengths are: the sequences' tiles of 128 keys, head by head, form one line, of which every workgroup takes an
+// equal piece.  A piece that is not a whole (sequence, head) leaves maximum, sum and output in the workspace; a second launch joins
+// them in a fixed order.  Each workgroup finds its piece from the lengths alone, so nothing has to be planned on the host, and a
+// captured call serves whatever lengths its arrays hold when it is replayed.
+//
+// In a workgroup each of the four waves takes 32 keys of a tile, on its own: K goes from memory to registers in the layout of the
+// matrix cores' operand (16 keys by quarter rows), V through the wave's own LDS, from which the transposing read takes columns.
+#include "hbl_internal.h"
+#include "paged_attention.h"
+
+namespace hbl {
+namespace {
+
+constexpr int kWaves = 4, kWaveKeys = 32, kTileKeys = kWaves * kWaveKeys, kThreads = 64 * kWaves;
+
+// Keys that some row of a sequence sees, from a multiple of 32 on, and their tiles.
+struct SeqWork {
+    SeqSpan span;
+    int rows_q;       // tokens looked at
+    int base, end;    // keys
+    int tiles;
+};
+__device__ __forceinline__ SeqWork seq_work(const AttentionArgs& a, int s) {
+    SeqWork w;
+    w.span = span_of(a.batch, a.cache.page_shift, a.T, s);
+    w.rows_q = w.span.n < a.max_q ? w.span.n : a.max_q;
+    w.base = w.end = w.tiles = 0;
+    const int before = w.span.total - w.span.n;   // position of the first token
+    const int first = before < 0 ? -before : 0;   // the first one that has a place
+    if (first < w.rows_q) {
+        const int prefix = a.prefix_lens ? a.prefix_lens[s] : 0;
+        const KeyRange lo = visible_keys(before + first, w.span.keys, a.window, prefix);
+        const KeyRange hi = visible_keys(before + w.rows_q - 1, w.span.keys, a.window, prefix);
+        if (hi.hi > lo.lo) {
+            w.base = lo.lo & ~(kWaveKeys - 1);
+            w.end = hi.hi;
+            w.tiles = (w.end - w.base + kTileKeys - 1) / kTileKeys;
+        }
+    }
+    return w;
+}
+
+// Tiles of the sequences before `mine` and of all of them; LDS: 2 * kThreads of int64.
+struct TileCount {
+    int64_t before, all;
+};
+__device__ __forceinline__ int64_t chunk_tiles(const AttentionArgs& a, int from, int to) {
+    int64_t n = 0;
+    for (int s = from; s < to; ++s) n += seq_work(a, s).tiles;
+    return n;
+}
+
+// The line of tiles cut into equal pieces.
+__device__ __forceinline__ int64_t piece_length(int64_t all_units, int pieces) {
+    const int64_t n = (all_units + pieces - 1) / pieces;
+    return n < 1 ? 1 : n;
+}
+
+// Inclusive sum over the workgroup's threads.
+__device__ __forceinline__ int64_t scan_threads(int64_t v, int64_t* lds) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int m = 1; m < 64; m <<= 1) {
+        const int64_t u = __shfl_up(v, m, 64);
+        if (lane >= m) v += u;
+    }
+    if (lane == 63) lds[wave] = v;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) v += lds[w];
+    return v;
+}
+
+__host__ __device__ constexpr int merge_stride(int d) { return d + 4; }
+__host__ __device__ constexpr size_t decode_lds(int d) {   // the waves' values, or 16 rows of four waves to join
+    const size_t v = (size_t)kWaves * kWaveKeys * d * 2, m = (size_t)kWaves * 16 * (merge_stride(d) + 2) * 4;
+    return v > m ? v : m;
+}
+
+// Partial results: per slot `rows` rows of d outputs, then per slot and row (maximum, sum).
+struct Partial {
+    float* o;
+    float2* ml;
+};
+__device__ __forceinline__ Partial partial_of(float* base, int slots, int rows, int d) {
+    return {base, reinterpret_cast<float2*>(base + (size_t)slots * rows * d)};
+}
+
+// Byte position of a 16-byte chunk in a wave's values in LDS.  Chunks are moved about by row so that the eight rows of which a
+// transposing read takes 32 bytes lie in different banks.
+template <int D>
+__device__ __forceinline__ int v_place(int row, int chunk) {
+    if constexpr (D == 64) return row * 128 + ((chunk ^ (2 * ((row >> 1) & 3))) << 4);
+    return row * (2 * D) + ((chunk ^ (2 * (row & 7))) << 4);
+}
+
+template <int D, int BITS, int NR>
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kernel(AttentionArgs a) {
+    constexpr int QW = D / 8;                                        // dwords of a lane's quarter of a query row
+    constexpr int G8 = D / 32;                                       // groups of 8 features in it
+    constexpr int KW = BITS == 3 ? (D == 64 ? 2 : D * 3 / 128) : D * BITS / 128;   // dwords of a lane's quarter of a key row
+    constexpr int VC = BITS == 16 ? 8 : 32;                          // values a lane loads at once
+    constexpr int VL = D / VC, VR = 64 / VL, VS = kWaveKeys / VR;    // lanes a row, rows a load, loads a tile
+    constexpr int VW = VC * BITS / 32;                               // dwords of it
+    constexpr float kBias = Codes<BITS>::kBias;
+    extern __shared__ __align__(16) char lds[];
+    __shared__ int64_t scan[kWaves];
+    __shared__ int64_t found[2];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, quarter = lane >> 4;
+    const int heads = a.cache.heads, page_mask = (1 << a.cache.page_shift) - 1;
+
+    // my piece of the line
+    const int per_thread = (a.batch.n_seqs + kThreads - 1) / kThreads;
+    const int my_from = min((int)threadIdx.x * per_thread, a.batch.n_seqs), my_to = min(my_from + per_thread, a.batch.n_seqs);
+    const int64_t mine = chunk_tiles(a, my_from, my_to);
+    const int64_t upto = scan_threads(mine, scan);
+    const int64_t all = scan[0] + scan[1] + scan[2] + scan[3];
+    const int64_t length = piece_length(all * heads, gridDim.x);
+    int64_t unit = blockIdx.x * length;
+    const int64_t last_unit = min(unit + length, all * heads);
+    if (unit >= last_unit) return;
+    {
+        int64_t at = (upto - mine) * heads;
+        if (unit >= at && unit < upto * heads) {
+            int s = my_from;
+            for (;; ++s) {
+                const int64_t n = (int64_t)seq_work(a, s).tiles * heads;
+                if (unit < at + n) break;
+                at += n;
+            }
+            found[0] = s;
+            found[1] = at;
+        }
+    }
+    __syncthreads();
+    int s = __builtin_amdgcn_readfirstlane((int)found[0]);
+    int64_t seq_unit = found[1];   // first unit of sequence s
+
+    char* const my_v = lds + wave * (kWaveKeys * D * 2);
+    const int slots = 2 * gridDim.x;
+    const Partial part = partial_of(a.partial, slots, 16 * NR, D);
+
+    while (unit < last_unit) {
+        const SeqWork w = seq_work(a, s);
+        if (unit >= seq_unit + (int64_t)w.tiles * heads) {   // (sequences without tiles are passed over)
+            seq_unit += (int64_t)w.tiles * heads;
+            ++s;
+            continue;
+        }
+        const int in_seq = (int)(unit - seq_unit), head = in_seq / w.tiles;
+        const int t0 = in_seq - head * w.tiles;
+        const int t1 = (int)min((int64_t)w.tiles, t0 + (last_unit - unit));
+        unit += t1 - t0;
+        const int rows = w.rows_q * a.group;
+        const int before = w.span.total - w.span.n;
+        const int prefix = a.prefix_lens ? a.prefix_lens[s] : 0;
+        const int32_t* table = a.batch.block_table + s * a.batch.table_stride;
+
+        // queries: column `col` of row tile r is row 16 r + col of (token, query head of the group)
+        uint32_t q[NR][QW];
+        float start[NR], slope[NR];
+        int position[NR];
+        KeyRange see[NR];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            const int row = 16 * r + col, token = row / a.group, h = head * a.group + row - token * a.group;
+            const bool live = row < rows;
+            float sum = 0.0f;
+#pragma unroll
+            for (int g = 0; g < G8; ++g) {
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (live)
+                    x = *reinterpret_cast<const uint4*>(a.q + (w.span.first + token) * a.q_stride + (int64_t)h * D + quarter * (D / 4) + 8 * g);
+                const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    // (feature i and i + 4 of the eight, or as they lie)
+                    q[r][4 * g + i] = !Codes<BITS>::kPaired ? y[i]
+                                                            : __builtin_amdgcn_perm(y[2 + (i >> 1)], y[i >> 1], (i & 1) ? 0x07060302u : 0x05040100u);
+                    sum += as_f(y[i] << 16) + as_f(y[i] & 0xFFFF0000u);
+                }
+            }
+            sum = join16(join32(sum, SumOf()), SumOf());
+            start[r] = -kBias * sum;
+            position[r] = live ? before + token : -1;
+            see[r] = visible_keys(position[r], w.span.keys, a.window, prefix);
+            slope[r] = a.slopes && live ? a.slopes[h] : 0.0f;
+        }
+        f32x4 o[NR][D / 16], psum[NR];
+        float m[NR], l[NR];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            m[r] = -INFINITY;
+            l[r] = 0.0f;
+            psum[r] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) o[r][i] = (f32x4){0, 0, 0, 0};
+        }
+
+        // pages of the two groups of 16 keys of a tile (a page holds whole groups); -1 where none is to be read
+        auto page_of = [&](int key) {
+            int p = -1;
+            if (key < w.end) p = table[key >> a.cache.page_shift];
+            return (uint32_t)p < (uint32_t)a.cache.n_pages ? p : -1;
+        };
+        auto row_of = [&](int page, int key) {
+            return (int64_t)page * a.cache.page_rows + ((int64_t)head << a.cache.page_shift) + (key & page_mask);
+        };
+        auto load_k = [&](int key0, const int* page, uint32_t (*k)[KW], f32x4* ks) {
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                ks[g] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < KW; ++i) k[g][i] = 0;
+                if (page[g] < 0) continue;
+                const int key = key0 + 16 * g;
+                const int64_t row = row_of(page[g], key);
+                if (key + col < w.end) {
+                    const uint8_t* at = a.cache.k + (row + col) * (D * BITS / 8);
+                    if constexpr (BITS == 3 && D == 64) {   // six bytes, from the dword on that holds the first
+                        load_dwords<2>(at + ((6 * quarter) & ~3), k[g]);
+                        if (quarter & 1) {
+                            k[g][0] = (k[g][0] >> 16) | (k[g][1] << 16);
+                            k[g][1] >>= 16;
+                        }
+                    } else {
+                        load_dwords<KW>(at + quarter * (KW * 4), k[g]);
+                    }
+                }
+                if constexpr (BITS != 16) load_dwords<4>(a.cache.k_scales + row + 4 * quarter, reinterpret_cast<uint32_t*>(&ks[g]));
+            }
+        };
+
+        uint32_t k[2][KW];
+        f32x4 ks[2];
+        int key0 = w.base + t0 * kTileKeys + wave * kWaveKeys;
+        const int key_end = min(w.end, w.base + t1 * kTileKeys);
+        int page[2] = {page_of(key0), page_of(key0 + 16)};
+        int next_page[2] = {page_of(key0 + kTileKeys), page_of(key0 + kTileKeys + 16)};
+        load_k(key0, page, k, ks);
+        for (; key0 < key_end; key0 += kTileKeys) {
+            // values of this tile
+            uint32_t v[VS][VW];
+            f32x4 vs[2];
+#pragma unroll
+            for (int i = 0; i < VS; ++i) {
+                const int in_tile = i * VR + lane / VL;
+                const int pg = in_tile < 16 ? page[0] : page[1];
+#pragma unroll
+                for (int j = 0; j < VW; ++j) v[i][j] = 0;
+                if (pg >= 0 && key0 + in_tile < w.end)
+                    load_dwords<VW>(a.cache.v + row_of(pg, key0 + in_tile) * (D * BITS / 8) + (lane % VL) * (VW * 4), v[i]);
+            }
+            if constexpr (BITS != 16) {
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    vs[g] = (f32x4){0, 0, 0, 0};
+                    if (page[g] >= 0) load_dwords<4>(a.cache.v_scales + row_of(page[g], key0 + 16 * g) + 4 * quarter, reinterpret_cast<uint32_t*>(&vs[g]));
+                }
+            }
+            // scores of two groups of 16 keys
+            f32x4 score[NR][2];
+#pragma unroll
+            for (int r = 0; r < NR; ++r)
+#pragma unroll
+                for (int g = 0; g < 2; ++g) score[r][g] = (f32x4){start[r], start[r], start[r], start[r]};
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int i = 0; i < G8; ++i) {
+                    const bf16x8 kk = __builtin_bit_cast(bf16x8, widen_codes<BITS>(k[g], i));
+#pragma unroll
+                    for (int r = 0; r < NR; ++r) {
+                        const bf16x8 qq = __builtin_bit_cast(bf16x8, (u32x4){q[r][4 * i], q[r][4 * i + 1], q[r][4 * i + 2], q[r][4 * i + 3]});
+                        score[r][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, qq, score[r][g], 0, 0, 0);
+                    }
+                }
+            f32x4 k_scale[2];
+#pragma unroll
+            for (int g = 0; g < 2; ++g) k_scale[g] = ks[g];
+            // keys of the next tile
+            const int here[2] = {page[0], page[1]};
+            page[0] = next_page[0];
+            page[1] = next_page[1];
+            load_k(key0 + kTileKeys, page, k, ks);
+            next_page[0] = page_of(key0 + 2 * kTileKeys);
+            next_page[1] = page_of(key0 + 2 * kTileKeys + 16);
+
+            bf16x8 p[NR];
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                float x[8];
+                bool seen[8];
+                float top = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int j = key0 + 16 * (i >> 2) + 4 * quarter + (i & 3);
+                    float y = score[r][i >> 2][i & 3];
+                    const float f = BITS == 16 ? a.scale : a.scale * k_scale[i >> 2][i & 3];
+                    if (a.softcap > 0.0f || a.slopes) {
+                        const int apart = position[r] - j;
+                        y = shaped_score(y * f, a.softcap, slope[r], apart < 0 ? -apart : apart);
+                    } else {
+                        y *= f * kLog2e;
+                    }
+                    seen[i] = j >= see[r].lo && j < see[r].hi && here[i >> 2] >= 0;
+                    x[i] = seen[i] ? y : -INFINITY;
+                    top = fmaxf(top, x[i]);
+                }
+                top = fmaxf(m[r], join16(join32(top, MaxOf()), MaxOf()));
+                if (__any(top > m[r])) {   // (rare after the first tiles)
+                    const float keep = top > m[r] ? __builtin_amdgcn_exp2f(m[r] - top) : 1.0f;
+                    l[r] *= keep;
+                    psum[r] *= keep;
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) o[r][i] *= keep;
+                    m[r] = top;
+                }
+                const float ref = top == -INFINITY ? 0.0f : top;
+                uint32_t packed[4];
+                float weight[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float e = __builtin_amdgcn_exp2f(x[i] - ref);
+                    l[r] += e;
+                    weight[i] = BITS == 16 ? e : (seen[i] ? e * vs[i >> 2][i & 3] : 0.0f);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) packed[i] = pack_bf16(weight[2 * i], weight[2 * i + 1]);
+                p[r] = __builtin_bit_cast(bf16x8, (u32x4){packed[0], packed[1], packed[2], packed[3]});
+            }
+
+            // values through LDS: rows in, columns out
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < VS; ++i) {
+                const int in_tile = i * VR + lane / VL;
+#pragma unroll
+                for (int g = 0; g < VC / 8; ++g)
+                    *reinterpret_cast<u32x4*>(my_v + v_place<D>(in_tile, (lane % VL) * (VC / 8) + g)) = widen_codes<BITS>(v[i], g);
+            }
+            asm volatile("" ::: "memory");
+            if constexpr (BITS != 16) {
+                const bf16x8 ones = __builtin_bit_cast(bf16x8, (u32x4){0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
+#pragma unroll
+                for (int r = 0; r < NR; ++r) psum[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[r], psum[r], 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                // lane (16 b + c) supplies row 4 b + c / 4, features 4 (c mod 4) on, and gets feature c of rows 4 b to 4 b + 3
+                uint32_t col_v[4];
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const int row = 16 * g + 4 * quarter + (col >> 2);
+                    const int byte = v_place<D>(row, 2 * i + ((col & 3) >> 1)) + 8 * (col & 1);
+                    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+                    const s16x4 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(my_v + byte));
+                    const uint2 u = __builtin_bit_cast(uint2, c);
+                    col_v[2 * g] = u.x;
+                    col_v[2 * g + 1] = u.y;
+                }
+                const bf16x8 vv = __builtin_bit_cast(bf16x8, (u32x4){col_v[0], col_v[1], col_v[2], col_v[3]});
+#pragma unroll
+                for (int r = 0; r < NR; ++r) o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, p[r], o[r][i], 0, 0, 0);
+            }
+        }
+
+        // the four waves' results joined, 16 rows at a time
+        float* const join_o = reinterpret_cast<float*>(lds);
+        float* const join_ml = join_o + kWaves * 16 * merge_stride(D);
+        const bool whole = t0 == 0 && t1 == w.tiles;
+        const int slot = 2 * (int)blockIdx.x + (t0 == 0);
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            __syncthreads();
+            const float sum = join16(join32(l[r], SumOf()), SumOf());
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int place = 16 * i + 4 * quarter + j;
+                    join_o[(wave * 16 + col) * merge_stride(D) + (place & ~7) + feature_at<BITS>(place & 7)] = o[r][i][j] - kBias * psum[r][j];
+                }
+            if (quarter == 0) {
+                join_ml[wave * 16 + col] = m[r];
+                join_ml[kWaves * 16 + wave * 16 + col] = sum;
+            }
+            __syncthreads();
+            const int in = threadIdx.x >> 4, row = 16 * r + in;
+            if (row < rows) {
+                float top = -INFINITY, total = 0.0f, f[kWaves];
+#pragma unroll
+                for (int x = 0; x < kWaves; ++x) top = fmaxf(top, join_ml[x * 16 + in]);
+#pragma unroll
+                for (int x = 0; x < kWaves; ++x) {
+                    f[x] = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(join_ml[x * 16 + in] - top);
+                    total += f[x] * join_ml[kWaves * 16 + x * 16 + in];
+                }
+                const float inverse = whole ? (total > 0.0f ? 1.0f / total : 0.0f) : 1.0f;
+                const int token = row / a.group, h = head * a.group + row - token * a.group;
+                if (!whole && (threadIdx.x & 15) == 0) part.ml[slot * (16 * NR) + row] = make_float2(top, total);
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) {
+                    const int at = 64 * i + 4 * (threadIdx.x & 15);
+                    float y[4] = {0, 0, 0, 0};
+#pragma unroll
+                    for (int x = 0; x < kWaves; ++x) {
+                        const f32x4 u = *reinterpret_cast<const f32x4*>(join_o + (x * 16 + in) * merge_stride(D) + at);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) y[j] += f[x] * u[j];
+                    }
+                    if (whole)
+                        *reinterpret_cast<uint2*>(a.out + (w.span.first + token) * a.out_stride + (int64_t)h * D + at) =
+                            make_uint2(pack_bf16(y[0] * inverse, y[1] * inverse), pack_bf16(y[2] * inverse, y[3] * inverse));
+                    else
+                        *reinterpret_cast<f32x4*>(part.o + ((size_t)slot * (16 * NR) + row) * D + at) = (f32x4){y[0], y[1], y[2], y[3]};
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Joins the partial results of one (sequence, key head) a workgroup; zeros where there was nothing to see.
+__global__ __launch_bounds__(kThreads) void paged_decode_join_kernel(AttentionArgs a, int pieces, int tile_rows) {
+    __shared__ int64_t sum[2];
+    const int heads = a.cache.heads, s = blockIdx.x / heads, head = blockIdx.x - s * heads;
+    if (threadIdx.x < 2) sum[threadIdx.x] = 0;
+    __syncthreads();
+    int64_t before = 0, all = 0;
+    for (int i = threadIdx.x; i < a.batch.n_seqs; i += kThreads) {
+        const int n = seq_work(a, i).tiles;
+        all += n;
+        before += i < s ? n : 0;
+    }
+    for (int m = 1; m < 64; m <<= 1) {
+        all += __shfl_xor(all, m, 64);
+        before += __shfl_xor(before, m, 64);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        atomicAdd(reinterpret_cast<unsigned long long*>(&sum[0]), (unsigned long long)before);
+        atomicAdd(reinterpret_cast<unsigned long long*>(&sum[1]), (unsigned long long)all);
+    }
+    __syncthreads();
+    const SeqWork w = seq_work(a, s);
+    const int64_t length = piece_length(sum[1] * heads, pieces);
+    const int64_t first_unit = sum[0] * heads + (int64_t)head * w.tiles;
+    const int g0 = (int)(first_unit / length), g1 = (int)((first_unit + w.tiles - 1) / length);
+    if (w.tiles > 0 && g0 == g1) return;   // one workgroup had it all
+    const int rows = w.rows_q * a.group;
+    const Partial part = partial_of(a.partial, 2 * pieces, tile_rows, a.d);
+    for (int i = threadIdx.x; i < rows * (a.d / 4); i += kThreads) {
+        const int row = i / (a.d / 4), at = 4 * (i - row * (a.d / 4));
+        const int token = row / a.group, h = head * a.group + row - token * a.group;
+        float top = -INFINITY, total = 0.0f;
+        f32x4 y = {0, 0, 0, 0};
+        if (w.tiles > 0) {
+            for (int g = g0; g <= g1; ++g) top = fmaxf(top, part.ml[(2 * g + (g == g0)) * tile_rows + row].x);
+            for (int g = g0; g <= g1 && top > -INFINITY; ++g) {
+                const size_t at_row = (size_t)(2 * g + (g == g0)) * tile_rows + row;
+                const float2 ml = part.ml[at_row];
+                const float f = __builtin_amdgcn_exp2f(ml.x - top);
+                total += f * ml.y;
+                y += f * *reinterpret_cast<const f32x4*>(part.o + at_row * a.d + at);
+            }
+        }
+        const float inverse = total > 0.0f ? 1.0f / total : 0.0f;
+        *reinterpret_cast<uint2*>(a.out + (w.span.first + token) * a.out_stride + (int64_t)h * a.d + at) =
+            make_uint2(pack_bf16(y[0] * inverse, y[1] * inverse), pack_bf16(y[2] * inverse, y[3] * inverse));
+    }
+}
+
+constexpr int kPieces = 512;
+
+template <int D, int BITS, int NR>
+int launch_form(const AttentionArgs& a, hipStream_t stream) {
+    constexpr size_t lds = decode_lds(D);
+    if (int rc = allow_dynamic_lds<&paged_decode_kernel<D, BITS, NR>, lds>(); rc != HBL_OK) return rc;
+    launch_kernel("paged_decode_kernel", paged_decode_kernel<D, BITS, NR>, dim3(kPieces), dim3(kThreads), lds, stream, a);
+    launch_kernel("paged_decode_join_kernel", paged_decode_join_kernel, dim3((unsigned)a.batch.n_seqs * (unsigned)a.cache.heads), dim3(kThreads), 0,
+                  stream, a, kPieces, 16 * NR);
+    return after_launch();
+}
+template <int D, int BITS>
+int launch_rows(const AttentionArgs& a, hipStream_t stream) {
+    return a.max_q * a.group <= 16 ? launch_form<D, BITS, 1>(a, stream) : launch_form<D, BITS, 2>(a, stream);
+}
+template <int D>
+int launch_bits(const AttentionArgs& a, int bits, hipStream_t stream) {
+    switch (bits) {
+        case 16: return launch_rows<D, 16>(a, stream);
+        case 8: return launch_rows<D, 8>(a, stream);
+        case 4: return launch_rows<D, 4>(a, stream);
+        default: return launch_rows<D, 3>(a, stream);
+    }
+}
+
+}  // namespace
+
+size_t paged_decode_workspace(int rows, int d) {
+    const int tile_rows = rows <= 16 ? 16 : 32;
+    return (size_t)2 * kPieces * tile_rows * (d + 2) * sizeof(float);
+}
+
+int launch_paged_decode(const AttentionArgs& a, int bits, hipStream_t stream) {
+    return a.d == 64 ? launch_bits<64>(a, bits, stream) : a.d == 128 ? launch_bits<128>(a, bits, stream) : launch_bits<256>(a, bits, stream);
+}
+
+}  // namespace hbl

@@ -24,7 +24,7 @@ LIB = os.path.join(PKG, "libhbitlinear.so")
 HOST_CALL = os.path.join(PKG, "_host_call" + sysconfig.get_config_var("EXT_SUFFIX"))   # (its name says for which Python)
 SOURCES = ["api.hip", "fwht_quant.hip", "ternary_setup.hip", "ternary_gemm.hip", "ternary_gemm_f6f4.hip", "mid_gemm.hip",
            "decode_gemm.hip", "fused_small.hip", "fused_bytes.hip", "kv_quant.hip", "rope.hip",
-           "paged_attention.hip", "paged_decode.hip"]
+           "paged_attention.hip", "paged_decode.hip", "paged_prefill.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

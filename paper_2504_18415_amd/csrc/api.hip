@@ -589,7 +589,7 @@ int check_attention_shape(const hbl_kv_cache* c, const hbl_kv_batch* b, int64_t 
     int rc = check_cache(c);
     if (rc == HBL_OK) rc = check_batch(b, T);
     if (rc != HBL_OK) return rc;
-    if (Hq < 1 || Hq > (1 << 16) || Hq % c->n_kv_heads != 0 || max_q_len < 1) return HBL_E_SHAPE;
+    if (Hq < 1 || Hq > (1 << 16) || Hq % c->n_kv_heads != 0 || max_q_len < 1 || T * Hq > 0x7FFFFFFF) return HBL_E_SHAPE;
     return HBL_OK;
 }
 

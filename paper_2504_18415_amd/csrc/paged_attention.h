@@ -42,6 +42,10 @@ constexpr int kDecodeRows = 32;
 size_t paged_decode_workspace(int rows, int d);
 int launch_paged_decode(const AttentionArgs& a, int bits, hipStream_t stream);
 
+// More rows (paged_prefill.hip).
+size_t paged_prefill_workspace(int64_t T, int n_seqs, int group, int heads, int d);
+int launch_paged_prefill(const AttentionArgs& a, int bits, hipStream_t stream);
+
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));

@@ -39,7 +39,7 @@ int launch_paged_attention(const AttentionArgs& a, int bits, void* workspace, hi
 
 // Few rows a key head (paged_decode.hip): at most kDecodeRows tokens times query heads of a group.
 constexpr int kDecodeRows = 32;
-size_t paged_decode_workspace(int rows, int d);
+size_t paged_decode_workspace(int rows, int d, int n_seqs, int heads);
 int launch_paged_decode(const AttentionArgs& a, int bits, hipStream_t stream);
 
 // More rows (paged_prefill.hip).
@@ -114,6 +114,13 @@ __device__ __forceinline__ void load_dwords(const void* p, uint32_t* w) {
     for (int i = 0; i < N; ++i) w[i] = c.w[i];
 }
 
+// An entry of the block table at an index that is the same for the whole wave, by a scalar load: it does not wait in line with the
+// vector loads in flight, as a vector load's result does (those of states that the next tile needs: 670 us were 690 for it).
+__device__ __forceinline__ int table_entry(const int32_t* table, int i) {
+    typedef const __attribute__((address_space(4))) int32_t* constant_int;
+    return ((constant_int)(uintptr_t)table)[__builtin_amdgcn_readfirstlane(i)];
+}
+
 // x op (the value of the lane 32, or 16, away), in every lane.
 template <typename Op>
 __device__ __forceinline__ float join32(float x, Op op) {
@@ -132,14 +139,14 @@ struct SumOf {
     __device__ float operator()(float a, float b) const { return a + b; }
 };
 
-// The score after cap and bias, in units of log 2.
-__device__ __forceinline__ float shaped_score(float s, float softcap, float slope, int distance) {
+// A score after the cap, if there is one (> 0), in units of log 2.
+__device__ __forceinline__ float capped_score(float s, float softcap) {
     if (softcap > 0.0f) {
         // tanh x = 1 - 2 / (e^(2x) + 1): the ends come out right where e^(2x) is 0 or infinite
         const float e = __builtin_amdgcn_exp2f(s * (2.0f * kLog2e / softcap));
         s = softcap * (1.0f - 2.0f * __builtin_amdgcn_rcpf(e + 1.0f));
     }
-    return (s - slope * (float)distance) * kLog2e;
+    return s * kLog2e;
 }
 
 }  // namespace hbl

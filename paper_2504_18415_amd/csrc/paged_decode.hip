@@ -15,6 +15,7 @@ namespace hbl {
 namespace {
 
 constexpr int kWaves = 4, kWaveKeys = 32, kTileKeys = kWaves * kWaveKeys, kThreads = 64 * kWaves;
+constexpr int kPieces = 512;   // workgroups: two for each of the 256 CUs
 
 // Keys that some row of a sequence sees, from a multiple of 32 on, and their tiles.
 struct SeqWork {
@@ -54,10 +55,7 @@ __device__ __forceinline__ int64_t chunk_tiles(const AttentionArgs& a, int from,
 }
 
 // The line of tiles cut into equal pieces.
-__device__ __forceinline__ int64_t piece_length(int64_t all_units, int pieces) {
-    const int64_t n = (all_units + pieces - 1) / pieces;
-    return n < 1 ? 1 : n;
-}
+__device__ __forceinline__ int64_t piece_length(int64_t all_units) { return all_units < 1 ? 1 : (all_units + kPieces - 1) / kPieces; }
 
 // Inclusive sum over the workgroup's threads.
 __device__ __forceinline__ int64_t scan_threads(int64_t v, int64_t* lds) {
@@ -78,13 +76,17 @@ __host__ __device__ constexpr size_t decode_lds(int d) {   // the waves' values,
     return v > m ? v : m;
 }
 
-// Partial results: per slot `rows` rows of d outputs, then per slot and row (maximum, sum).
+// Workspace: two slots a workgroup of `rows` rows of d outputs; (maximum, sum) of those rows; for every (sequence, key head) with tiles
+// the first and the last workgroup that has some, noted by the first.
 struct Partial {
     float* o;
     float2* ml;
 };
-__device__ __forceinline__ Partial partial_of(float* base, int slots, int rows, int d) {
-    return {base, reinterpret_cast<float2*>(base + (size_t)slots * rows * d)};
+__device__ __forceinline__ Partial partial_of(float* base, int rows, int d) {
+    return {base, reinterpret_cast<float2*>(base + (size_t)2 * kPieces * rows * d)};
+}
+__device__ __forceinline__ int2* held_by(float* base, int rows, int d) {
+    return reinterpret_cast<int2*>(base + (size_t)2 * kPieces * rows * (d + 2));
 }
 
 // Byte position of a 16-byte chunk in a wave's values in LDS.  Chunks are moved about by row so that the eight rows of which a
@@ -117,7 +119,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
     const int64_t mine = chunk_tiles(a, my_from, my_to);
     const int64_t upto = scan_threads(mine, scan);
     const int64_t all = scan[0] + scan[1] + scan[2] + scan[3];
-    const int64_t length = piece_length(all * heads, gridDim.x);
+    const int64_t length = piece_length(all * heads);
     int64_t unit = blockIdx.x * length;
     const int64_t last_unit = min(unit + length, all * heads);
     if (unit >= last_unit) return;
@@ -139,8 +141,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
     int64_t seq_unit = found[1];   // first unit of sequence s
 
     char* const my_v = lds + wave * (kWaveKeys * D * 2);
-    const int slots = 2 * gridDim.x;
-    const Partial part = partial_of(a.partial, slots, 16 * NR, D);
+    const Partial part = partial_of(a.partial, 16 * NR, D);
 
     while (unit < last_unit) {
         const SeqWork w = seq_work(a, s);
@@ -200,10 +201,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
         }
 
         // pages of the two groups of 16 keys of a tile (a page holds whole groups); -1 where none is to be read
-        auto page_of = [&](int key) {
-            int p = -1;
-            if (key < w.end) p = table[key >> a.cache.page_shift];
-            return (uint32_t)p < (uint32_t)a.cache.n_pages ? p : -1;
+        auto page_of = [&](int key) {   // (beyond the end: the last key's entry is read, and not used)
+            const int p = table_entry(table, (key < w.end ? key : w.end - 1) >> a.cache.page_shift);
+            return key < w.end && (uint32_t)p < (uint32_t)a.cache.n_pages ? p : -1;
         };
         auto row_of = [&](int page, int key) {
             return (int64_t)page * a.cache.page_rows + ((int64_t)head << a.cache.page_shift) + (key & page_mask);
@@ -300,8 +300,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
                     float y = score[r][i >> 2][i & 3];
                     const float f = BITS == 16 ? a.scale : a.scale * k_scale[i >> 2][i & 3];
                     if (a.softcap > 0.0f || a.slopes) {
-                        const int apart = position[r] - j;
-                        y = shaped_score(y * f, a.softcap, slope[r], apart < 0 ? -apart : apart);
+                        y = capped_score(y * f, a.softcap) - slope[r] * kLog2e * fabsf((float)(position[r] - j));
                     } else {
                         y *= f * kLog2e;
                     }
@@ -371,6 +370,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
         float* const join_o = reinterpret_cast<float*>(lds);
         float* const join_ml = join_o + kWaves * 16 * merge_stride(D);
         const bool whole = t0 == 0 && t1 == w.tiles;
+        if (t0 == 0 && threadIdx.x == 0)   // (unit is the end of this piece: what is left of the tiles follows, `length` a workgroup)
+            held_by(a.partial, 16 * NR, D)[s * heads + head] =
+                make_int2((int)blockIdx.x, (int)blockIdx.x + (int)((w.tiles - t1 + length - 1) / length));
         const int slot = 2 * (int)blockIdx.x + (t0 == 0);
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
@@ -424,47 +426,29 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
 }
 
 // Joins the partial results of one (sequence, key head) a workgroup; zeros where there was nothing to see.
-__global__ __launch_bounds__(kThreads) void paged_decode_join_kernel(AttentionArgs a, int pieces, int tile_rows) {
-    __shared__ int64_t sum[2];
+__global__ __launch_bounds__(kThreads) void paged_decode_join_kernel(AttentionArgs a, int tile_rows) {
     const int heads = a.cache.heads, s = blockIdx.x / heads, head = blockIdx.x - s * heads;
-    if (threadIdx.x < 2) sum[threadIdx.x] = 0;
-    __syncthreads();
-    int64_t before = 0, all = 0;
-    for (int i = threadIdx.x; i < a.batch.n_seqs; i += kThreads) {
-        const int n = seq_work(a, i).tiles;
-        all += n;
-        before += i < s ? n : 0;
-    }
-    for (int m = 1; m < 64; m <<= 1) {
-        all += __shfl_xor(all, m, 64);
-        before += __shfl_xor(before, m, 64);
-    }
-    if ((threadIdx.x & 63) == 0) {
-        atomicAdd(reinterpret_cast<unsigned long long*>(&sum[0]), (unsigned long long)before);
-        atomicAdd(reinterpret_cast<unsigned long long*>(&sum[1]), (unsigned long long)all);
-    }
-    __syncthreads();
     const SeqWork w = seq_work(a, s);
-    const int64_t length = piece_length(sum[1] * heads, pieces);
-    const int64_t first_unit = sum[0] * heads + (int64_t)head * w.tiles;
-    const int g0 = (int)(first_unit / length), g1 = (int)((first_unit + w.tiles - 1) / length);
-    if (w.tiles > 0 && g0 == g1) return;   // one workgroup had it all
+    const int2 held = held_by(a.partial, tile_rows, a.d)[blockIdx.x];   // (nobody notes anything where there are no tiles)
+    const int g0 = w.tiles > 0 ? held.x : 0, g1 = w.tiles > 0 ? held.y : -1;
+    if (g0 == g1) return;   // one workgroup had it all
     const int rows = w.rows_q * a.group;
-    const Partial part = partial_of(a.partial, 2 * pieces, tile_rows, a.d);
+    const Partial part = partial_of(a.partial, tile_rows, a.d);
     for (int i = threadIdx.x; i < rows * (a.d / 4); i += kThreads) {
         const int row = i / (a.d / 4), at = 4 * (i - row * (a.d / 4));
         const int token = row / a.group, h = head * a.group + row - token * a.group;
         float top = -INFINITY, total = 0.0f;
         f32x4 y = {0, 0, 0, 0};
-        if (w.tiles > 0) {
-            for (int g = g0; g <= g1; ++g) top = fmaxf(top, part.ml[(2 * g + (g == g0)) * tile_rows + row].x);
-            for (int g = g0; g <= g1 && top > -INFINITY; ++g) {
-                const size_t at_row = (size_t)(2 * g + (g == g0)) * tile_rows + row;
-                const float2 ml = part.ml[at_row];
-                const float f = __builtin_amdgcn_exp2f(ml.x - top);
-                total += f * ml.y;
-                y += f * *reinterpret_cast<const f32x4*>(part.o + at_row * a.d + at);
-            }
+#pragma unroll 4
+        for (int g = g0; g <= g1; ++g) {
+            const size_t at_row = (size_t)(2 * g + (g == g0)) * tile_rows + row;
+            const float2 ml = part.ml[at_row];
+            const f32x4 o = *reinterpret_cast<const f32x4*>(part.o + at_row * a.d + at);
+            const float to = fmaxf(top, ml.x), ref = to == -INFINITY ? 0.0f : to;
+            const float keep = __builtin_amdgcn_exp2f(top - ref), f = __builtin_amdgcn_exp2f(ml.x - ref);
+            total = total * keep + f * ml.y;
+            y = y * keep + f * o;
+            top = to;
         }
         const float inverse = total > 0.0f ? 1.0f / total : 0.0f;
         *reinterpret_cast<uint2*>(a.out + (w.span.first + token) * a.out_stride + (int64_t)h * a.d + at) =
@@ -472,15 +456,13 @@ __global__ __launch_bounds__(kThreads) void paged_decode_join_kernel(AttentionAr
     }
 }
 
-constexpr int kPieces = 512;
-
 template <int D, int BITS, int NR>
 int launch_form(const AttentionArgs& a, hipStream_t stream) {
     constexpr size_t lds = decode_lds(D);
     if (int rc = allow_dynamic_lds<&paged_decode_kernel<D, BITS, NR>, lds>(); rc != HBL_OK) return rc;
     launch_kernel("paged_decode_kernel", paged_decode_kernel<D, BITS, NR>, dim3(kPieces), dim3(kThreads), lds, stream, a);
     launch_kernel("paged_decode_join_kernel", paged_decode_join_kernel, dim3((unsigned)a.batch.n_seqs * (unsigned)a.cache.heads), dim3(kThreads), 0,
-                  stream, a, kPieces, 16 * NR);
+                  stream, a, 16 * NR);
     return after_launch();
 }
 template <int D, int BITS>
@@ -499,9 +481,9 @@ int launch_bits(const AttentionArgs& a, int bits, hipStream_t stream) {
 
 }  // namespace
 
-size_t paged_decode_workspace(int rows, int d) {
+size_t paged_decode_workspace(int rows, int d, int n_seqs, int heads) {
     const int tile_rows = rows <= 16 ? 16 : 32;
-    return (size_t)2 * kPieces * tile_rows * (d + 2) * sizeof(float);
+    return (size_t)2 * kPieces * tile_rows * (d + 2) * sizeof(float) + (size_t)n_seqs * heads * sizeof(int2);
 }
 
 int launch_paged_decode(const AttentionArgs& a, int bits, hipStream_t stream) {

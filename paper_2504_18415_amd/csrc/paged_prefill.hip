@@ -35,61 +35,18 @@ struct Item {
     SeqSpan span;
     int rows;      // of the sequence (tokens looked at times group)
 };
-__device__ __forceinline__ int row_tiles(const AttentionArgs& a, int s) {
-    const SeqSpan span = span_of(a.batch, a.cache.page_shift, a.T, s);
-    const int n = span.n < a.max_q ? span.n : a.max_q;
-    return (int)(((int64_t)n * a.group + kRows - 1) / kRows);
-}
-// The row tiles of all sequences and where the rank-th is (the last tiles first: they see most keys).  false: there are not so many.
-struct Search {
-    int sums[kWaves], found[2], all;
-};
-__device__ __forceinline__ int count_row_tiles(const AttentionArgs& a, Search* lds, int from, int to, int& before) {
-    int mine = 0;
-    for (int s = from; s < to; ++s) mine += row_tiles(a, s);
-    int v = mine;
-    for (int m = 1; m < 64; m <<= 1) {
-        const int u = __shfl_up(v, m, 64);
-        if ((int)(threadIdx.x & 63) >= m) v += u;
-    }
-    if ((threadIdx.x & 63) == 63) lds->sums[threadIdx.x >> 6] = v;
-    __syncthreads();
-    int all = 0;
-    before = v - mine;
-    for (int w = 0; w < kWaves; ++w) {
-        if (w < (int)(threadIdx.x >> 6)) before += lds->sums[w];
-        all += lds->sums[w];
-    }
-    return all;
-}
-__device__ __forceinline__ void thread_share(const AttentionArgs& a, int& from, int& to) {
-    const int per = (a.batch.n_seqs + kThreads - 1) / kThreads;
-    from = min((int)threadIdx.x * per, a.batch.n_seqs);
-    to = min(from + per, a.batch.n_seqs);
-}
-__device__ __forceinline__ Item find_item(const AttentionArgs& a, Search* lds, int from, int to, int before, int index) {
-    for (int s = from, at = before; s < to; ++s) {
-        const int n = row_tiles(a, s);
-        if (index >= at && index < at + n) {
-            lds->found[0] = s;
-            lds->found[1] = index - at;
-        }
-        at += n;
-    }
-    __syncthreads();
-    Item it;
-    it.s = __builtin_amdgcn_readfirstlane(lds->found[0]);
-    it.tile = __builtin_amdgcn_readfirstlane(lds->found[1]);
-    it.span = span_of(a.batch, a.cache.page_shift, a.T, it.s);
+__device__ __forceinline__ Item item_of(const AttentionArgs& a, int s, int tile) {
+    Item it{s, tile, span_of(a.batch, a.cache.page_shift, a.T, s), 0};
     it.rows = (it.span.n < a.max_q ? it.span.n : a.max_q) * a.group;
     return it;
 }
+__device__ __forceinline__ int row_tiles(const AttentionArgs& a, int s) { return (item_of(a, s, 0).rows + kRows - 1) / kRows; }
 
-// Keys that some row of the tile sees, from a multiple of 16 on.
+// Keys that some row of the tile sees, from a multiple of the tile of keys on.
 struct TileKeys {
     int base, end;
 };
-__device__ __forceinline__ TileKeys tile_keys(const AttentionArgs& a, const Item& it, int prefix) {
+__device__ __forceinline__ TileKeys tile_keys(const AttentionArgs& a, const Item& it, int prefix, int tile) {
     const int before = it.span.total - it.span.n;
     int first = it.tile * kRows / a.group;
     const int last = min((it.tile + 1) * kRows, it.rows) - 1;
@@ -98,8 +55,127 @@ __device__ __forceinline__ TileKeys tile_keys(const AttentionArgs& a, const Item
     const KeyRange lo = visible_keys(before + first, it.span.keys, a.window, prefix);
     const KeyRange hi = visible_keys(before + last / a.group, it.span.keys, a.window, prefix);
     if (hi.hi <= lo.lo) return {0, 0};
-    return {lo.lo & ~15, hi.hi};
+    return {lo.lo & ~(tile - 1), hi.hi};
 }
+// How the work is cut: a unit is a row tile and a part of its keys.  All row tiles of a sequence have the same number of parts,
+// their keys over `length` tiles, rounded up.
+//
+// With few units there is none for some CUs, and with a few more than the chip holds at once the last ones run alone: the length is the
+// one that takes the shortest time in one round of the chip, or in two.  The lengths, known on the device only, decide; every
+// workgroup looks for it by itself, a candidate a thread.
+constexpr int kMostSplitSeqs = 128, kMostKeyTiles = 1 << 20;
+// Parts of so many tiles of keys at a length: the quotient rounded up, at most 64 (an estimate by floats, the same wherever it is made).
+__device__ __forceinline__ int parts_at(int tiles, int length, float inverse) {
+    return tiles <= length ? 1 : min(64, (int)((float)(tiles - 1) * inverse) + 1);
+}
+struct Search {
+    int tiles[kMostSplitSeqs], keys[kMostSplitSeqs];   // of a sequence: row tiles; tiles of keys of the last of them
+    int sums[kWaves], best[2 * kWaves], found[3];
+};
+struct Unit {
+    int s, tile, part, parts;
+    int all;   // units of a key head
+};
+// Unit `rank` of a key head (a function of it, which may need `all`); s < 0: there is none.  `round`: units that run at once, 0: parts are whole.
+template <typename Rank>
+__device__ __forceinline__ Unit find_unit(const AttentionArgs& a, Search* lds, int tile, int round, int most, Rank rank_of) {
+    const int n_seqs = a.batch.n_seqs, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    int length = 0x7FFFFFFF;
+    if (round > 0) {
+        if ((int)threadIdx.x < n_seqs) {
+            const int n = row_tiles(a, threadIdx.x);
+            TileKeys k{0, 0};
+            if (n > 0) k = tile_keys(a, item_of(a, threadIdx.x, n - 1), a.prefix_lens ? a.prefix_lens[threadIdx.x] : 0, tile);
+            lds->tiles[threadIdx.x] = n;
+            lds->keys[threadIdx.x] = (k.end - k.base + tile - 1) / tile;
+        }
+        __syncthreads();
+        uint32_t work = 0;   // (at most `most` row tiles' keys: it fits)
+        for (int s = 0; s < n_seqs; ++s) work += (uint32_t)lds->tiles[s] * (uint32_t)min(lds->keys[s], kMostKeyTiles);
+        // candidates: from an even share of a round (of two) on in steps of a 32nd of it
+        const int rounds = 1 + wave / (kWaves / 2), step = (wave % (kWaves / 2)) * 64 + lane;
+        const float share = (float)work * (float)a.cache.heads / (float)(rounds * round);
+        int at = max(4, (int)fminf(share * (1.0f + step * (1.0f / 32.0f)) + 1.0f, 1e9f));
+        const float inverse = 1.0f / (float)at;
+        int units = 0, longest = 0;
+        for (int s = 0; s < n_seqs; ++s) {
+            const int parts = parts_at(lds->keys[s], at, inverse);
+            units += min(lds->tiles[s] * parts, 1 << 20);
+            longest = max(longest, lds->tiles[s] > 0 ? (int)((float)lds->keys[s] / (float)parts) : 0);
+        }
+        // (a unit's beginning and end cost about as much as four tiles)
+        const bool fits = (int64_t)units * a.cache.heads <= min(rounds * round, most);
+        int cost = fits ? rounds * (longest + 4) : 0x7FFFFFFF;
+        for (int m = 1; m < 64; m <<= 1) {
+            const int c = __shfl_xor(cost, m, 64), l = __shfl_xor(at, m, 64);
+            if (c < cost || (c == cost && l > at)) {
+                cost = c;
+                at = l;
+            }
+        }
+        if (lane == 0) {
+            lds->best[2 * wave] = cost;
+            lds->best[2 * wave + 1] = at;
+        }
+        __syncthreads();
+        int least = 0x7FFFFFFF;
+        for (int w = 0; w < kWaves; ++w)
+            if (lds->best[2 * w] < least) {
+                least = lds->best[2 * w];
+                length = lds->best[2 * w + 1];
+            }
+    }
+    // where the sequences' units begin
+    const int per = (n_seqs + kThreads - 1) / kThreads;
+    const int from = min((int)threadIdx.x * per, n_seqs), to = min(from + per, n_seqs);
+    const float inverse = 1.0f / (float)length;
+    auto parts_of = [&](int s) { return round > 0 ? parts_at(lds->keys[s], length, inverse) : 1; };
+    int mine = 0;
+    for (int s = from; s < to; ++s) mine += row_tiles(a, s) * parts_of(s);
+    int v = mine;
+    for (int m = 1; m < 64; m <<= 1) {
+        const int u = __shfl_up(v, m, 64);
+        if (lane >= m) v += u;
+    }
+    if (lane == 63) lds->sums[wave] = v;
+    if (threadIdx.x == 0) lds->found[0] = -1;
+    __syncthreads();
+    Unit unit{-1, 0, 0, 1, 0};
+    int at = v - mine;
+    for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) at += lds->sums[w];
+        unit.all += lds->sums[w];
+    }
+    const int rank = rank_of(unit.all);
+    for (int s = from; s < to; ++s) {
+        const int parts = parts_of(s), n = row_tiles(a, s) * parts;
+        if (rank >= at && rank < at + n) {
+            lds->found[0] = s;
+            lds->found[1] = rank - at;
+            lds->found[2] = parts;
+        }
+        at += n;
+    }
+    __syncthreads();
+    unit.s = __builtin_amdgcn_readfirstlane(lds->found[0]);
+    unit.parts = __builtin_amdgcn_readfirstlane(lds->found[2]);
+    if (unit.s >= 0) {
+        const int in_seq = __builtin_amdgcn_readfirstlane(lds->found[1]);
+        unit.tile = in_seq / unit.parts;
+        unit.part = in_seq - unit.tile * unit.parts;
+    }
+    return unit;
+}
+
+// A row tile that was cut, as its first part's workgroup notes it: the slots of its parts are heads apart from `slot` on.
+struct Done {
+    int s, tile, head, slot, parts;
+};
+// Workspace: outputs [most][kRows][d], maxima and sums [most][kRows], notes [workgroups].
+__device__ __forceinline__ Done* done_of(const AttentionArgs& a, int most) {
+    return reinterpret_cast<Done*>(a.partial + (size_t)most * kRows * (a.d + 2));
+}
+
 struct Part {
     int from, to;   // tiles of keys
 };
@@ -107,8 +183,13 @@ __device__ __forceinline__ Part part_of(int tiles, int part, int parts) {
     return {(int)((int64_t)tiles * part / parts), (int)((int64_t)tiles * (part + 1) / parts)};
 }
 
-template <int D, int BITS, bool SHAPED>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kernel(AttentionArgs a, int parts) {
+// What is done to scores: nothing but the scale; a cap so low (kLowCap) that weights need no reference, the largest being e^cap; a bias
+// by distance; a cap of any size and a bias, if any.
+constexpr int kScaled = 0, kCapped = 1, kBiased = 2, kShaped = 3;
+constexpr float kLowCap = 40.0f;   // e^40 < 2^58, and e^-40 times a scale of 10^-20 is a normal number still
+
+template <int D, int BITS, int SHAPE>
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kernel(AttentionArgs a, int round, int most) {
     constexpr int TK = kTile<D>, KB = TK / 32;              // blocks of 32 keys
     constexpr int RW = TK / kWaves;                         // rows of a tile that a wave loads (16 bits)
     constexpr int RI = 512 / D, NI = RW / RI;               // rows a load, loads
@@ -123,26 +204,31 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
     const int col = lane & 31, half = lane >> 5;
     const int heads = a.cache.heads, page_mask = (1 << a.cache.page_shift) - 1;
 
-    int from, to, before_me;
-    thread_share(a, from, to);
-    const int items = count_row_tiles(a, &search, from, to, before_me);
-    // workgroups go round the eight XCDs: where it divides, each works through whole heads, whose keys its cache then holds
-    int head, rank;
-    if (heads % 8 == 0) {
-        const int in_xcd = blockIdx.x >> 3;
-        if (items == 0) return;
-        head = (int)(blockIdx.x & 7) + 8 * (in_xcd / (items * parts));
-        rank = in_xcd % (items * parts);
-    } else {
-        head = blockIdx.x % heads;
-        rank = blockIdx.x / heads;
-    }
-    if (head >= heads || rank >= items * parts) return;
-    const int part = rank % parts, index = items - 1 - rank / parts;
-    const Item it = find_item(a, &search, from, to, before_me, index);
+    // Workgroups go round the eight XCDs: where the heads divide among them each works through whole heads, whose keys its cache then
+    // holds.  The last row tiles, which see most keys, come first.
+    int head = 0, rank = 0;
+    const Unit unit = find_unit(a, &search, TK, round, most, [&](int all) {
+        if (heads % 8 == 0) {
+            const int in_xcd = blockIdx.x >> 3;
+            head = all > 0 ? (int)(blockIdx.x & 7) + 8 * (in_xcd / all) : heads;
+            rank = all > 0 ? all - 1 - in_xcd % all : -1;
+        } else {
+            head = blockIdx.x % heads;
+            rank = all - 1 - (int)(blockIdx.x / heads);
+        }
+        return rank;
+    });
+    const bool mine_at_all = head < heads && unit.s >= 0;
+    // (what this workgroup takes, for the second launch: nothing, or a part of a row tile that is whole where it has one part)
+    if (most > 0 && threadIdx.x == 0)
+        done_of(a, most)[blockIdx.x] = mine_at_all && unit.part == 0 && unit.parts > 1
+                                           ? Done{unit.s, unit.tile, head, rank * heads + head, unit.parts}
+                                           : Done{-1, 0, 0, 0, 0};
+    if (!mine_at_all) return;
+    const Item it = item_of(a, unit.s, unit.tile);
     const int prefix = a.prefix_lens ? a.prefix_lens[it.s] : 0;
-    const TileKeys keys = tile_keys(a, it, prefix);
-    const Part mine = part_of((keys.end - keys.base + TK - 1) / TK, part, parts);
+    const TileKeys keys = tile_keys(a, it, prefix, TK);
+    const Part mine = part_of((keys.end - keys.base + TK - 1) / TK, unit.part, unit.parts);
     const int32_t* table = a.batch.block_table + it.s * a.batch.table_stride;
 
     // my column's row: queries, range
@@ -150,7 +236,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
     const bool live = row < it.rows;
     const int position = live ? it.span.total - it.span.n + token : -1;
     const KeyRange see = visible_keys(position, it.span.keys, a.window, prefix);
-    const float slope = SHAPED && a.slopes && live ? a.slopes[h] : 0.0f;
+    const float slope = SHAPE >= kBiased && a.slopes && live ? a.slopes[h] : 0.0f;
     bf16x8 q[D / 16];
     float start = 0.0f;
     {
@@ -173,8 +259,11 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
         }
         if constexpr (CODES) start = -kBias * join32(sum, SumOf());
     }
-    // (at least the smallest normal number: minus infinity, in hidden places, has to stay what it is)
-    const float scale = fabsf(a.scale), scale2 = fmaxf(scale * kLog2e, 1.17549435e-38f);
+    // What a sum of products is multiplied by: to be a score in units of log 2, the exponent of the cap's e^(2 s / cap) in them, a score.
+    // Codes get it with their scales.  (At least the smallest normal number: minus infinity, in hidden places, has to stay that.)
+    const float cap2 = a.softcap * kLog2e, scale = fabsf(a.scale);
+    const float factor = SHAPE == kScaled ? fmaxf(scale * kLog2e, 1.17549435e-38f) : SHAPE == kCapped ? scale * (2.0f * kLog2e / a.softcap) : SHAPE == kBiased ? scale * kLog2e : scale;
+    const float step = CODES || SHAPE != kScaled ? 1.0f : factor;
     // keys that all of the wave's rows see, and those that some does
     int all_lo = live ? see.lo : 0, all_hi = live ? see.hi : 0x7FFFFFFF, any_lo = see.hi > see.lo ? see.lo : 0x7FFFFFFF, any_hi = see.hi > see.lo ? see.hi : 0;
     for (int m = 1; m < 32; m <<= 1) {
@@ -193,12 +282,35 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
     for (int i = 0; i < 16; ++i) psum[i] = 0.0f;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) o[i] = psum;
-    float m = -INFINITY, l = 0.0f;
+    float m = SHAPE == kCapped ? 0.0f : -INFINITY, l = 0.0f;
 
-    auto page_of = [&](int key) {   // of a group of 16 keys; -1: none
+    auto page_of = [&](int key) {   // -1: none
         int p = -1;
         if (key < keys.end) p = table[key >> a.cache.page_shift];
         return (uint32_t)p < (uint32_t)a.cache.n_pages ? p : -1;
+    };
+    // the same of a group of 16 keys, for a whole wave (beyond the end: the last key's entry is read, and not used)
+    auto group_page = [&](int key) {
+        const int p = table_entry(table, (key < keys.end ? key : keys.end - 1) >> a.cache.page_shift);
+        return key < keys.end && (uint32_t)p < (uint32_t)a.cache.n_pages ? p : -1;
+    };
+    // Pages of a tile, looked up a tile before its states are fetched: that of the wave's own rows (16 bits), and a bit for each group
+    // of 16 keys that has none.  (Tiles begin at multiples of their length: a page that is as long holds all of one.)
+    struct Pages {
+        int own, absent;
+    };
+    const bool one_page = (1 << a.cache.page_shift) >= TK;
+    auto pages_of = [&](int key0) {
+        Pages p{-1, 0};
+        if (one_page && key0 + TK <= keys.end) {
+            p.own = group_page(key0);
+            p.absent = p.own < 0 ? (1 << (TK / 16)) - 1 : 0;
+        } else {
+            if (BITS == 16) p.own = group_page((key0 + wave * RW) & ~15);
+#pragma unroll
+            for (int g = 0; g < TK / 16; ++g) p.absent |= group_page(key0 + 16 * g) < 0 ? 1 << g : 0;
+        }
+        return p;
     };
     auto row_of = [&](int page, int key) {
         return (int64_t)page * a.cache.page_rows + ((int64_t)head << a.cache.page_shift) + (key & page_mask);
@@ -215,21 +327,23 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
         offset[0][i] = k_place<D>(r, at) - wave * RW * (2 * D);
         offset[1][i] = v_place<D>(r, at) - wave * RW * (2 * D);
     }
-    auto fetch16 = [&](int key0, int buffer) {
-        const int first = key0 + wave * RW, page = __builtin_amdgcn_readfirstlane(page_of(first));
-        const int64_t row0 = page < 0 ? 0 : row_of(page, first);
+    auto fetch16 = [&](int key0, int page, int buffer) {
+        const int first = key0 + wave * RW;
+        const uint32_t to = (uint32_t)(uintptr_t)(lds_void*)(side(buffer, 0) + wave * RW * (2 * D));
+        const int64_t row0 = page < 0 ? 0 : row_of(page, first) * (2 * D);
+        if (page >= 0 && first + RW <= keys.end) {   // (one question a tile: asked at every load, the branches took longer than the loads)
 #pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            const uint8_t* from_row = (which ? a.cache.v : a.cache.k) + row0 * (2 * D);
+            for (int i = 0; i < 2 * NI; ++i)
+                gemm::lds_dma16(to + (i / NI) * SIDE + (i % NI) * 1024, (i < NI ? a.cache.k : a.cache.v) + row0, offset[i / NI][i % NI]);
+        } else {
+#pragma unroll 1
+            for (int which = 0; which < 2; ++which) {
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const uint32_t to = (uint32_t)(uintptr_t)(lds_void*)(side(buffer, which) + (wave * RW + i * RI) * (2 * D));
-                if (page >= 0 && first + RW <= keys.end) {
-                    gemm::lds_dma16(to, from_row, offset[which][i]);
-                } else if (page >= 0 && first + i * RI + lane / (D / 8) < keys.end) {
-                    gemm::lds_dma16(to, from_row, offset[which][i]);
-                } else {   // (each lane's bytes land in the lane's place, whichever of the two copies takes them there)
-                    gemm::lds_dma16(to, no_state, 16 * (lane % (D / 8)));
+                for (int i = 0; i < NI; ++i) {   // each lane's bytes land in the lane's place, whichever of the two copies takes them there
+                    if (page >= 0 && first + i * RI + lane / (D / 8) < keys.end)
+                        gemm::lds_dma16(to + which * SIDE + i * 1024, (which ? a.cache.v : a.cache.k) + row0, which ? offset[1][i] : offset[0][i]);
+                    else
+                        gemm::lds_dma16(to + which * SIDE + i * 1024, no_state, 16 * (lane % (D / 8)));
                 }
             }
         }
@@ -252,7 +366,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
         raw_scale = 0.0f;
         if ((int)threadIdx.x < 2 * TK) {
             const int k = key0 + (int)(threadIdx.x % TK), p = page_of(k);
-            if (p >= 0) raw_scale = ((int)threadIdx.x < TK ? a.cache.k_scales : a.cache.v_scales)[row_of(p, k)];
+            if (p >= 0) raw_scale = (int)threadIdx.x < TK ? a.cache.k_scales[row_of(p, k)] * factor : a.cache.v_scales[row_of(p, k)];
         }
     };
     auto store_codes = [&](int buffer) {
@@ -269,13 +383,16 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
         if ((int)threadIdx.x < 2 * TK) scales[buffer * 2 * TK + threadIdx.x] = raw_scale;
     };
 
+    Pages pages{-1, 0}, next_pages{-1, 0};
     if (mine.from < mine.to) {
         const int key0 = keys.base + mine.from * TK;
+        pages = pages_of(key0);
+        next_pages = pages_of(key0 + TK);
         if constexpr (CODES) {
             fetch_codes(key0);
             store_codes(0);
         } else {
-            fetch16(key0, 0);
+            fetch16(key0, pages.own, 0);
         }
     }
     gemm::wait_loads_then_barrier<0>();
@@ -284,12 +401,18 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
         const bool more = t + 1 < mine.to;
         if (more) {
             if constexpr (CODES) fetch_codes(key0 + TK);
-            else fetch16(key0 + TK, buffer ^ 1);
+            else fetch16(key0 + TK, next_pages.own, buffer ^ 1);
         }
+        const int absent = pages.absent;
+        pages = next_pages;
+        next_pages = pages_of(key0 + 2 * TK);
         if (key0 < any_hi && key0 + TK > any_lo) {
             const char* const kt = side(buffer, 0);
             char* const vt = side(buffer, 1);
             f32x16 score[KB];
+            // (a wave that multiplies goes before the other one of its SIMD, which then takes weights: 584 -> 572 us for an 8192-token
+            // prompt of 32 heads; the same around the values 587)
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int b = 0; b < KB; ++b) {
 #pragma unroll
@@ -300,30 +423,35 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
                     score[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, q[i], score[b], 0, 0, 0);
                 }
             }
+            // four operands are on their way from LDS while one is multiplied (left to itself the compiler waits for each: 2 to 4 % longer)
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+            for (int i = 0; i < KB * D / 16 - 4; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+            __builtin_amdgcn_s_setprio(0);
             // element 4 j + i of block b is key 32 b + 8 j + 4 half + i
-            if constexpr (CODES || SHAPED) {
+            if constexpr (CODES || SHAPE != kScaled) {
+                const float apart = (float)(position - key0 - 4 * half);
 #pragma unroll
                 for (int b = 0; b < KB; ++b)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        f32x4 ks = {1, 1, 1, 1};
+                        f32x4 ks = {factor, factor, factor, factor};
                         if constexpr (CODES) ks = *reinterpret_cast<const f32x4*>(scales + buffer * 2 * TK + 32 * b + 8 * j + 4 * half);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            float x = score[b][4 * j + i];
-                            if constexpr (CODES) x *= ks[i];
-                            if constexpr (SHAPED) {
-                                const int apart = position - (key0 + 32 * b + 8 * j + 4 * half + i);
-                                x = shaped_score(x * scale, a.softcap, slope, apart < 0 ? -apart : apart);
-                            }
+                            float x = score[b][4 * j + i] * ks[i];
+                            if constexpr (SHAPE == kCapped)   // cap (1 - 2 / (e^(2 s / cap) + 1)), in units of log 2
+                                x = __builtin_fmaf(-2.0f * cap2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x) + 1.0f), cap2);
+                            if constexpr (SHAPE == kShaped) x = capped_score(x, a.softcap);
+                            if constexpr (SHAPE >= kBiased) x = __builtin_fmaf(-slope * kLog2e, fabsf(apart - (float)(32 * b + 8 * j + i)), x);
                             score[b][4 * j + i] = x;
                         }
                     }
             }
-            int absent = 0;   // groups of 16 keys without a page
-#pragma unroll
-            for (int g = 0; g < TK / 16; ++g)
-                if (page_of(key0 + 16 * g) < 0) absent |= 1 << g;
             const bool plain = key0 >= all_lo && key0 + TK <= all_hi && absent == 0;
             if (!plain) {
 #pragma unroll
@@ -334,24 +462,26 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
                         if (j < see.lo || j >= see.hi || (absent >> (2 * b + (i >> 3)) & 1)) score[b][i] = -INFINITY;
                     }
             }
-            float top = -INFINITY;
+            float ref = 0.0f;
+            if constexpr (SHAPE != kCapped) {
+                float top = -INFINITY;
 #pragma unroll
-            for (int b = 0; b < KB; ++b)
+                for (int b = 0; b < KB; ++b)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, score[b][i]);
-            const float unit = SHAPED ? 1.0f : scale2;
-            top = join32(top, MaxOf());
-            top = top == -INFINITY ? top : top * unit;
-            // The reference stays until a maximum is far above it: weights up to 2^8 are as good as those up to 1.
-            if (__any(top > m + 8.0f || (m == -INFINITY && top > m))) {
-                const float to = fmaxf(m, top), keep = to > m ? __builtin_amdgcn_exp2f(m - to) : 1.0f;
-                l *= keep;
-                if constexpr (CODES) psum *= keep;
+                    for (int i = 0; i < 16; ++i) top = fmaxf(top, score[b][i]);
+                top = join32(top, MaxOf());
+                top = top == -INFINITY ? top : top * step;
+                // The reference stays until a maximum is far above it: weights up to 2^8 are as good as those up to 1.
+                if (__any(top > m + 8.0f || (m == -INFINITY && top > m))) {
+                    const float to = fmaxf(m, top), keep = to > m ? __builtin_amdgcn_exp2f(m - to) : 1.0f;
+                    l *= keep;
+                    if constexpr (CODES) psum *= keep;
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i) o[i] *= keep;
-                m = to;
+                    for (int i = 0; i < D / 32; ++i) o[i] *= keep;
+                    m = to;
+                }
+                ref = m == -INFINITY ? 0.0f : -m;
             }
-            const float ref = m == -INFINITY ? 0.0f : -m;
             bf16x8 p[KB][2];
 #pragma unroll
             for (int b = 0; b < KB; ++b) {
@@ -362,7 +492,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float x = score[b][4 * j + i];
-                        e[i] = __builtin_amdgcn_exp2f(SHAPED ? x + ref : __builtin_fmaf(x, unit, ref));
+                        e[i] = __builtin_amdgcn_exp2f(CODES || SHAPE != kScaled ? x + ref : __builtin_fmaf(x, step, ref));
                         l += e[i];
                     }
                     if constexpr (CODES) {
@@ -407,13 +537,12 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
     }
 
     const float sum = join32(l, SumOf());
-    const bool whole = parts == 1;
+    const bool whole = unit.parts == 1;
     const float inverse = whole ? (sum > 0.0f ? 1.0f / sum : 0.0f) : 1.0f;
     if (!live) return;
-    const size_t slot_row = ((size_t)(index * heads + head) * parts + part) * kRows + wave * 32 + col;
-    const size_t slots = (size_t)items * heads * parts;
+    const size_t slot_row = ((size_t)rank * heads + head) * kRows + wave * 32 + col;
     float* const part_o = a.partial;
-    float2* const part_ml = reinterpret_cast<float2*>(a.partial + slots * kRows * D);
+    float2* const part_ml = reinterpret_cast<float2*>(a.partial + (size_t)most * kRows * D);
     if (!whole && half == 0) part_ml[slot_row] = make_float2(m, sum);
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
@@ -439,34 +568,33 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
         }
 }
 
-// Joins the parts of one row tile and key head a workgroup.
-__global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(AttentionArgs a, int parts, int tile) {
-    __shared__ Search search;
-    const int heads = a.cache.heads, index = blockIdx.x / heads, head = blockIdx.x - index * heads;
-    int from, to, before_me;
-    thread_share(a, from, to);
-    const int items = count_row_tiles(a, &search, from, to, before_me);
-    if (index >= items) return;
-    const Item it = find_item(a, &search, from, to, before_me, index);
-    const TileKeys keys = tile_keys(a, it, a.prefix_lens ? a.prefix_lens[it.s] : 0);
+// Joins the parts of a quarter of a row tile (32 rows) of a key head a workgroup.
+__global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(AttentionArgs a, int tile, int most) {
+    const int quarter = blockIdx.x & 3, heads = a.cache.heads;
+    const Done unit = done_of(a, most)[blockIdx.x >> 2];
+    if (unit.s < 0) return;
+    const int head = unit.head;
+    const Item it = item_of(a, unit.s, unit.tile);
+    const TileKeys keys = tile_keys(a, it, a.prefix_lens ? a.prefix_lens[it.s] : 0, tile);
     const int tiles = (keys.end - keys.base + tile - 1) / tile;
-    const size_t slots = (size_t)items * heads * parts, slot0 = ((size_t)index * heads + head) * parts;
-    const float2* const part_ml = reinterpret_cast<const float2*>(a.partial + slots * kRows * a.d);
-    const int rows = min(kRows, it.rows - it.tile * kRows);
+    const float2* const part_ml = reinterpret_cast<const float2*>(a.partial + (size_t)most * kRows * a.d);
+    const int rows = min(32, it.rows - it.tile * kRows - 32 * quarter);
     for (int i = threadIdx.x; i < rows * (a.d / 4); i += kThreads) {
-        const int r = i / (a.d / 4), at = 4 * (i - r * (a.d / 4)), row = it.tile * kRows + r;
+        const int r = 32 * quarter + i / (a.d / 4), at = 4 * (i % (a.d / 4)), row = it.tile * kRows + r;
         const int token = row / a.group, h = head * a.group + row - token * a.group;
         float top = -INFINITY, total = 0.0f;
         f32x4 y = {0, 0, 0, 0};
-        for (int x = 0; x < parts; ++x) top = fmaxf(top, part_ml[(slot0 + x) * kRows + r].x);
-        for (int x = 0; x < parts && top > -INFINITY; ++x) {
-            const Part p = part_of(tiles, x, parts);
+        for (int x = 0; x < unit.parts; ++x) {
+            const Part p = part_of(tiles, x, unit.parts);
             if (p.from == p.to) continue;
-            const size_t at_row = (slot0 + x) * kRows + r;
+            const size_t at_row = ((size_t)unit.slot + (size_t)x * heads) * kRows + r;
             const float2 ml = part_ml[at_row];
-            const float f = __builtin_amdgcn_exp2f(ml.x - top);
-            total += f * ml.y;
-            y += f * *reinterpret_cast<const f32x4*>(a.partial + at_row * a.d + at);
+            const f32x4 o = *reinterpret_cast<const f32x4*>(a.partial + at_row * a.d + at);
+            if (ml.x == -INFINITY) continue;
+            const float to = fmaxf(top, ml.x), keep = __builtin_amdgcn_exp2f(top - to), f = __builtin_amdgcn_exp2f(ml.x - to);
+            total = total * keep + f * ml.y;
+            y = y * keep + f * o;
+            top = to;
         }
         const float inverse = total > 0.0f ? 1.0f / total : 0.0f;
         *reinterpret_cast<uint2*>(a.out + (it.span.first + token) * a.out_stride + (int64_t)h * a.d + at) =
@@ -479,31 +607,41 @@ int64_t most_row_tiles(int64_t T, int n_seqs, int group) {
     const int64_t rows = T * group, seqs = n_seqs < T ? n_seqs : T;
     return rows / kRows + seqs;
 }
-// Parts of the keys: until there are two workgroups for each of the 256 CUs, and at most eight.
-int key_parts(int64_t T, int n_seqs, int group, int heads) {
-    const int64_t wgs = most_row_tiles(T, n_seqs, group) * heads;
-    int parts = 1;
-    while (parts < 8 && wgs * parts * 2 <= 640) parts *= 2;
-    return parts;
+// Workgroups that the chip's 256 CUs hold at once, and units that a call with parts may have (a bit less than two rounds: the
+// workspace then is 66 MB at most).
+constexpr int round_of(int d) { return d == 256 ? 256 : 512; }
+constexpr int most_units(int d) { return d == 256 ? 500 : 1000; }
+// Whether keys are cut: if there may be units for it.
+bool cut_keys(int64_t T, int n_seqs, int group, int heads, int d) {
+    return n_seqs <= kMostSplitSeqs && most_row_tiles(T, n_seqs, group) * heads < most_units(d);
 }
 
 template <int D, int BITS>
+constexpr size_t lds_of() { return (size_t)4 * kTile<D> * D * 2 + (BITS == 16 ? 0 : 4 * kTile<D> * sizeof(float)); }
+
+template <int D, int BITS, int SHAPE>
+int launch_shape(const AttentionArgs& a, unsigned wgs, int round, int most, hipStream_t stream) {
+    constexpr size_t lds = lds_of<D, BITS>();
+    if (int rc = allow_dynamic_lds<&paged_prefill_kernel<D, BITS, SHAPE>, lds>(); rc != HBL_OK) return rc;
+    launch_kernel("paged_prefill_kernel", paged_prefill_kernel<D, BITS, SHAPE>, dim3(wgs), dim3(kThreads), lds, stream, a, round, most);
+    return HBL_OK;
+}
+template <int D, int BITS>
 int launch_form(const AttentionArgs& a, hipStream_t stream) {
-    constexpr size_t lds = (size_t)4 * kTile<D> * D * 2 + (BITS == 16 ? 0 : 4 * kTile<D> * sizeof(float));
-    const int heads = a.cache.heads, parts = key_parts(a.T, a.batch.n_seqs, a.group, heads);
-    const int64_t tiles = most_row_tiles(a.T, a.batch.n_seqs, a.group);
-    const int64_t wgs = tiles * parts * heads;
+    const int heads = a.cache.heads;
+    const bool cut = cut_keys(a.T, a.batch.n_seqs, a.group, heads, D);
+    const int most = cut ? most_units(D) : 0, round = cut ? round_of(D) : 0;
+    // (heads in eights: each XCD has a head's units one after the other, so the grid is whole eights)
+    const int64_t wgs = cut ? (most + 7) / 8 * 8 : most_row_tiles(a.T, a.batch.n_seqs, a.group) * heads;
     if (wgs > 0x7FFFFFFF) return HBL_E_SHAPE;
-    if (a.softcap > 0.0f || a.slopes) {
-        if (int rc = allow_dynamic_lds<&paged_prefill_kernel<D, BITS, true>, lds>(); rc != HBL_OK) return rc;
-        launch_kernel("paged_prefill_kernel", paged_prefill_kernel<D, BITS, true>, dim3((unsigned)wgs), dim3(kThreads), lds, stream, a, parts);
-    } else {
-        if (int rc = allow_dynamic_lds<&paged_prefill_kernel<D, BITS, false>, lds>(); rc != HBL_OK) return rc;
-        launch_kernel("paged_prefill_kernel", paged_prefill_kernel<D, BITS, false>, dim3((unsigned)wgs), dim3(kThreads), lds, stream, a, parts);
-    }
-    if (parts > 1)
-        launch_kernel("paged_prefill_join_kernel", paged_prefill_join_kernel, dim3((unsigned)(tiles * heads)), dim3(kThreads), 0, stream, a, parts,
-                      kTile<D>);
+    int rc;
+    if (a.slopes && a.softcap == 0.0f) rc = launch_shape<D, BITS, kBiased>(a, (unsigned)wgs, round, most, stream);
+    else if (a.slopes || a.softcap > kLowCap) rc = launch_shape<D, BITS, kShaped>(a, (unsigned)wgs, round, most, stream);
+    else if (a.softcap > 0.0f) rc = launch_shape<D, BITS, kCapped>(a, (unsigned)wgs, round, most, stream);
+    else rc = launch_shape<D, BITS, kScaled>(a, (unsigned)wgs, round, most, stream);
+    if (rc != HBL_OK) return rc;
+    if (cut)
+        launch_kernel("paged_prefill_join_kernel", paged_prefill_join_kernel, dim3((unsigned)(4 * wgs)), dim3(kThreads), 0, stream, a, kTile<D>, most);
     return after_launch();
 }
 template <int D>
@@ -519,8 +657,7 @@ int launch_bits(const AttentionArgs& a, int bits, hipStream_t stream) {
 }  // namespace
 
 size_t paged_prefill_workspace(int64_t T, int n_seqs, int group, int heads, int d) {
-    const int parts = key_parts(T, n_seqs, group, heads);
-    return parts == 1 ? 0 : (size_t)(most_row_tiles(T, n_seqs, group) * heads * parts) * kRows * (d + 2) * sizeof(float);
+    return cut_keys(T, n_seqs, group, heads, d) ? (size_t)most_units(d) * kRows * (d + 2) * sizeof(float) + (most_units(d) + 8) * sizeof(Done) : 0;
 }
 
 int launch_paged_prefill(const AttentionArgs& a, int bits, hipStream_t stream) {

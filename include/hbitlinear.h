@@ -415,6 +415,7 @@ int hbl_kv_append(const hbl_kv_cache* cache, const hbl_kv_batch* batch, const vo
  * weights are rounded to bf16 for the product with the values.
  *   q, out          [T, n_q_heads, d] bf16 with strides in values as for hbl_rope; they must not overlap
  *   max_q_len       at least the new tokens of any sequence (those beyond it are left as they were)
+ *   sizes           T n_q_heads < 2^31, n_seqs n_kv_heads table_width page_size < 2^38
  *   window >= 0;  slopes device [n_q_heads] fp32 or NULL;  prefix_lens device [n_seqs] int32 or NULL
  *   workspace       device, >= hbl_paged_attention_workspace_bytes(same arguments), 256-byte aligned; nothing in it has to
  *                   start at a value; calls that may overlap need one each

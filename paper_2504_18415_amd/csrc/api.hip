@@ -581,8 +581,10 @@ PagedCache paged_cache(const hbl_kv_cache* c) {
     while ((1 << shift) < c->page_size) ++shift;
     return {static_cast<uint8_t*>(c->k), static_cast<uint8_t*>(c->v), c->k_scales, c->v_scales, c->page_rows, (int)c->n_pages, c->n_kv_heads, shift};
 }
-PagedBatch paged_batch(const hbl_kv_batch* b) {
-    return {b->q_starts, b->kv_lens, b->block_table, b->table_stride, b->n_seqs, b->table_width};
+PagedBatch paged_batch(const hbl_kv_batch* b, const hbl_kv_cache* c) {
+    // (a cache without pages has no keys: nothing looks for one)
+    const int64_t keys = c->n_pages > 0 ? (int64_t)b->table_width * c->page_size : 0;
+    return {b->q_starts, b->kv_lens, b->block_table, b->table_stride, b->n_seqs, (int)(keys < 0x7FFFFFFF ? keys : 0x7FFFFFFF)};
 }
 // Sizes of an attention call (nothing here is read through a pointer).
 int check_attention_shape(const hbl_kv_cache* c, const hbl_kv_batch* b, int64_t T, int64_t Hq, int64_t max_q_len) {
@@ -590,6 +592,8 @@ int check_attention_shape(const hbl_kv_cache* c, const hbl_kv_batch* b, int64_t 
     if (rc == HBL_OK) rc = check_batch(b, T);
     if (rc != HBL_OK) return rc;
     if (Hq < 1 || Hq > (1 << 16) || Hq % c->n_kv_heads != 0 || max_q_len < 1 || T * Hq > 0x7FFFFFFF) return HBL_E_SHAPE;
+    // (tiles of keys are counted in 32 bits)
+    if ((double)b->n_seqs * c->n_kv_heads * b->table_width * c->page_size >= (double)((int64_t)1 << 38)) return HBL_E_SHAPE;
     return HBL_OK;
 }
 
@@ -651,7 +655,7 @@ int hbl_kv_append(const hbl_kv_cache* cache, const hbl_kv_batch* batch, const vo
         if ((rc = check_heads(q_out, q_out_dtype, T, n_q_heads, cache->d, q_out_stride)) != HBL_OK) return rc;
         if (q == q_out && (x_dtype != q_out_dtype || q_stride != q_out_stride)) return HBL_E_SHAPE;
     }
-    return launch_kv_append(paged_cache(cache), cache->bits, cache->d, paged_batch(batch), k, k_stride, v, v_stride, x_dtype, T, q,
+    return launch_kv_append(paged_cache(cache), cache->bits, cache->d, paged_batch(batch, cache), k, k_stride, v, v_stride, x_dtype, T, q,
                             n_q_heads, q_stride, q_out, q_out_dtype, q_out_stride, freqs, rot_dim, layout, magnitude, eps,
                             static_cast<hipStream_t>(stream));
 }
@@ -682,7 +686,7 @@ int hbl_paged_attention(const void* q, int64_t T, int64_t n_q_heads, int64_t q_s
     a.q_stride = q_stride;
     a.out_stride = out_stride;
     a.cache = paged_cache(cache);
-    a.batch = paged_batch(batch);
+    a.batch = paged_batch(batch, cache);
     a.slopes = slopes;
     a.prefix_lens = prefix_lens;
     a.scale = scale;
@@ -697,8 +701,8 @@ int hbl_paged_attention(const void* q, int64_t T, int64_t n_q_heads, int64_t q_s
 
 int hbl_test_kv_rows(const hbl_kv_cache* cache, const hbl_kv_batch* batch, int64_t T, int seq, int64_t* rows, int n_rows, int* span) {
     const PagedCache c = paged_cache(cache);
-    const PagedBatch b = paged_batch(batch);
-    const SeqSpan s = span_of(b, c.page_shift, (int)T, seq);
+    const PagedBatch b = paged_batch(batch, cache);
+    const SeqSpan s = span_of(b, (int)T, seq);
     span[0] = s.first;
     span[1] = s.n;
     span[2] = s.keys;

@@ -24,7 +24,8 @@ struct PagedBatch {
     const int32_t* kv_lens;       // [n_seqs]
     const int32_t* block_table;   // [n_seqs][table_stride]
     int64_t table_stride;
-    int n_seqs, table_width;
+    int n_seqs;
+    int capacity;                 // keys that a row of the table has pages for (up to 2^31 - 1)
 };
 
 // Sequence s as the kernels take it: tokens [first, first + n) inside the call's T, `keys` inside its row of the table.  `total` is
@@ -32,17 +33,17 @@ struct PagedBatch {
 struct SeqSpan {
     int first, n, keys, total;
 };
-__host__ __device__ inline SeqSpan make_span(int start, int end, int total, int T, int64_t capacity) {
+__host__ __device__ inline SeqSpan make_span(int start, int end, int total, int T, int capacity) {
     SeqSpan r;
     r.first = start < 0 ? 0 : (start < T ? start : T);
     const int last = end < r.first ? r.first : (end < T ? end : T);
     r.n = last - r.first;
     r.total = total < 0 ? 0 : total;
-    r.keys = (int64_t)r.total < capacity ? r.total : (int)capacity;
+    r.keys = r.total < capacity ? r.total : capacity;
     return r;
 }
-__host__ __device__ inline SeqSpan span_of(const PagedBatch& b, int page_shift, int T, int s) {
-    return make_span(b.q_starts[s], b.q_starts[s + 1], b.kv_lens[s], T, (int64_t)b.table_width << page_shift);
+__host__ __device__ inline SeqSpan span_of(const PagedBatch& b, int T, int s) {
+    return make_span(b.q_starts[s], b.q_starts[s + 1], b.kv_lens[s], T, b.capacity);
 }
 // First row of a page for one head, or -1 if the table's entry names no page.
 __host__ __device__ inline int64_t page_row(const PagedCache& c, int page, int head) {

@@ -72,36 +72,47 @@ __host__ __device__ constexpr int feature_at(int i) {
     return Codes<BITS>::kPaired ? (i >> 1) + 4 * (i & 1) : i;
 }
 
-// 8 codes of a row, from the dwords that hold them, as 8 bf16 (value + kBias) in the converted order.  `g`: which eight of the chunk.
+// The two constants of the conversion, kept in registers: the compiler then has one instruction (and, or) for each pair of values,
+// where literals take two.
 template <int BITS>
-__device__ __forceinline__ u32x4 widen_codes(const uint32_t* w, int g) {
-    if constexpr (BITS == 16) {
-        return (u32x4){w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]};
-    } else if constexpr (BITS == 8) {
-        u32x4 r;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t x = w[2 * g + i];
-            // (the float of an integer below 256 has its upper half's bits only: that half is the bf16)
-            const uint32_t a = as_u((float)(x & 0xFFu)), b = as_u((float)((x >> 8) & 0xFFu)), c = as_u((float)((x >> 16) & 0xFFu)), e = as_u((float)(x >> 24));
-            r[2 * i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
-            r[2 * i + 1] = __builtin_amdgcn_perm(e, c, 0x07060302u);
+struct Widen {
+    uint32_t mask, base;
+    __device__ __forceinline__ Widen() {
+        mask = BITS == 4 ? 0x00780078u : 0x00700070u;
+        base = BITS == 4 ? 0x41804180u : 0x41004100u;   // 16.0, of which a mantissa step is 1/8; 8.0, of which it is 1/16
+        if constexpr (Codes<BITS>::kPaired) {
+            asm("" : "+s"(mask));
+            asm("" : "+v"(base));
         }
-        return r;
-    } else if constexpr (BITS == 4) {
-        const uint32_t x = w[g];   // 0x4180 = 16.0, of which a mantissa step is 1/8
-        return (u32x4){((x << 3) & 0x00780078u) | 0x41804180u, ((x >> 1) & 0x00780078u) | 0x41804180u,
-                       ((x >> 5) & 0x00780078u) | 0x41804180u, ((x >> 9) & 0x00780078u) | 0x41804180u};
-    } else {
-        // 24 bits from bit 24 g of the chunk on; codes 4 to 7 are moved up to bit 16
-        const uint32_t lo = w[(3 * g) >> 2];
-        const int at = (3 * g) & 3;
-        const uint32_t x = at == 0 ? lo : at == 1 ? lo >> 8 : __builtin_amdgcn_alignbyte(w[((3 * g) >> 2) + 1], lo, at);
-        const uint32_t y = (x & 0xFFFu) | ((x & 0xFFF000u) << 4);   // 0x4100 = 8.0, of which a mantissa step is 1/16
-        return (u32x4){((y << 4) & 0x00700070u) | 0x41004100u, ((y << 1) & 0x00700070u) | 0x41004100u,
-                       ((y >> 2) & 0x00700070u) | 0x41004100u, ((y >> 5) & 0x00700070u) | 0x41004100u};
     }
-}
+    // 8 codes of a row, from the dwords that hold them, as 8 bf16 (value + kBias) in the converted order.  `g`: which eight of the chunk.
+    __device__ __forceinline__ u32x4 operator()(const uint32_t* w, int g) const {
+        if constexpr (BITS == 16) {
+            return (u32x4){w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]};
+        } else if constexpr (BITS == 8) {
+            u32x4 r;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t x = w[2 * g + i];
+                // (the float of an integer below 256 has its upper half's bits only: that half is the bf16)
+                const uint32_t a = as_u((float)(x & 0xFFu)), b = as_u((float)((x >> 8) & 0xFFu)), c = as_u((float)((x >> 16) & 0xFFu)), e = as_u((float)(x >> 24));
+                r[2 * i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+                r[2 * i + 1] = __builtin_amdgcn_perm(e, c, 0x07060302u);
+            }
+            return r;
+        } else if constexpr (BITS == 4) {
+            const uint32_t x = w[g];
+            return (u32x4){((x << 3) & mask) | base, ((x >> 1) & mask) | base, ((x >> 5) & mask) | base, ((x >> 9) & mask) | base};
+        } else {
+            // 24 bits from bit 24 g of the chunk on; codes 4 to 7 are moved up to bit 16
+            const uint32_t lo = w[(3 * g) >> 2];
+            const int at = (3 * g) & 3;
+            const uint32_t x = at == 0 ? lo : at == 1 ? lo >> 8 : __builtin_amdgcn_alignbyte(w[((3 * g) >> 2) + 1], lo, at);
+            const uint32_t y = (x & 0xFFFu) | ((x & 0xFFF000u) << 4);
+            return (u32x4){((y << 4) & mask) | base, ((y << 1) & mask) | base, ((y >> 2) & mask) | base, ((y >> 5) & mask) | base};
+        }
+    }
+};
 
 // N dwords from a 4-byte aligned address.
 template <int N>
@@ -119,6 +130,14 @@ __device__ __forceinline__ void load_dwords(const void* p, uint32_t* w) {
 __device__ __forceinline__ int table_entry(const int32_t* table, int i) {
     typedef const __attribute__((address_space(4))) int32_t* constant_int;
     return ((constant_int)(uintptr_t)table)[__builtin_amdgcn_readfirstlane(i)];
+}
+
+// A value that is the same in all lanes, where the compiler does not see it (it came through LDS): what follows from it then is scalar.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// span_of() of a sequence that is the same for the whole wave.
+__device__ __forceinline__ SeqSpan uniform_span(const PagedBatch& b, int T, int s) {
+    return make_span(table_entry(b.q_starts, s), table_entry(b.q_starts, s + 1), table_entry(b.kv_lens, s), T, b.capacity);
 }
 
 // x op (the value of the lane 32, or 16, away), in every lane.

@@ -24,15 +24,16 @@ struct SeqWork {
     int base, end;    // keys
     int tiles;
 };
+template <bool UNIFORM = false>
 __device__ __forceinline__ SeqWork seq_work(const AttentionArgs& a, int s) {
     SeqWork w;
-    w.span = span_of(a.batch, a.cache.page_shift, a.T, s);
+    w.span = UNIFORM ? uniform_span(a.batch, a.T, s) : span_of(a.batch, a.T, s);
     w.rows_q = w.span.n < a.max_q ? w.span.n : a.max_q;
     w.base = w.end = w.tiles = 0;
     const int before = w.span.total - w.span.n;   // position of the first token
     const int first = before < 0 ? -before : 0;   // the first one that has a place
     if (first < w.rows_q) {
-        const int prefix = a.prefix_lens ? a.prefix_lens[s] : 0;
+        const int prefix = !a.prefix_lens ? 0 : UNIFORM ? table_entry(a.prefix_lens, s) : a.prefix_lens[s];
         const KeyRange lo = visible_keys(before + first, w.span.keys, a.window, prefix);
         const KeyRange hi = visible_keys(before + w.rows_q - 1, w.span.keys, a.window, prefix);
         if (hi.hi > lo.lo) {
@@ -44,24 +45,21 @@ __device__ __forceinline__ SeqWork seq_work(const AttentionArgs& a, int s) {
     return w;
 }
 
-// Tiles of the sequences before `mine` and of all of them; LDS: 2 * kThreads of int64.
-struct TileCount {
-    int64_t before, all;
-};
-__device__ __forceinline__ int64_t chunk_tiles(const AttentionArgs& a, int from, int to) {
-    int64_t n = 0;
+// Tiles of some sequences.
+__device__ __forceinline__ int chunk_tiles(const AttentionArgs& a, int from, int to) {
+    int n = 0;
     for (int s = from; s < to; ++s) n += seq_work(a, s).tiles;
     return n;
 }
 
 // The line of tiles cut into equal pieces.
-__device__ __forceinline__ int64_t piece_length(int64_t all_units) { return all_units < 1 ? 1 : (all_units + kPieces - 1) / kPieces; }
+__device__ __forceinline__ int piece_length(int all_units) { return all_units < 1 ? 1 : (all_units + kPieces - 1) / kPieces; }
 
 // Inclusive sum over the workgroup's threads.
-__device__ __forceinline__ int64_t scan_threads(int64_t v, int64_t* lds) {
+__device__ __forceinline__ int scan_threads(int v, int* lds) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int m = 1; m < 64; m <<= 1) {
-        const int64_t u = __shfl_up(v, m, 64);
+        const int u = __shfl_up(v, m, 64);
         if (lane >= m) v += u;
     }
     if (lane == 63) lds[wave] = v;
@@ -97,18 +95,17 @@ __device__ __forceinline__ int v_place(int row, int chunk) {
     return row * (2 * D) + ((chunk ^ (2 * (row & 7))) << 4);
 }
 
-template <int D, int BITS, int NR>
+template <int D, int BITS, int NR, bool SHAPED>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kernel(AttentionArgs a) {
     constexpr int QW = D / 8;                                        // dwords of a lane's quarter of a query row
     constexpr int G8 = D / 32;                                       // groups of 8 features in it
     constexpr int KW = BITS == 3 ? (D == 64 ? 2 : D * 3 / 128) : D * BITS / 128;   // dwords of a lane's quarter of a key row
-    constexpr int VC = BITS == 16 ? 8 : 32;                          // values a lane loads at once
-    constexpr int VL = D / VC, VR = 64 / VL, VS = kWaveKeys / VR;    // lanes a row, rows a load, loads a tile
-    constexpr int VW = VC * BITS / 32;                               // dwords of it
+    constexpr int VL = BITS == 16 ? D / 8 : 4, VR = 64 / VL;         // lanes a row of values, rows a load (16 or less: of one page)
+    constexpr int VS = kWaveKeys / VR, VW = BITS == 16 ? 4 : KW;     // loads a tile, dwords of one
+    constexpr int V8 = BITS == 16 ? 1 : G8;                          // groups of 8 features in it
     constexpr float kBias = Codes<BITS>::kBias;
     extern __shared__ __align__(16) char lds[];
-    __shared__ int64_t scan[kWaves];
-    __shared__ int64_t found[2];
+    __shared__ int scan[kWaves], found[2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
     const int heads = a.cache.heads, page_mask = (1 << a.cache.page_shift) - 1;
@@ -116,19 +113,20 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
     // my piece of the line
     const int per_thread = (a.batch.n_seqs + kThreads - 1) / kThreads;
     const int my_from = min((int)threadIdx.x * per_thread, a.batch.n_seqs), my_to = min(my_from + per_thread, a.batch.n_seqs);
-    const int64_t mine = chunk_tiles(a, my_from, my_to);
-    const int64_t upto = scan_threads(mine, scan);
-    const int64_t all = scan[0] + scan[1] + scan[2] + scan[3];
-    const int64_t length = piece_length(all * heads);
-    int64_t unit = blockIdx.x * length;
-    const int64_t last_unit = min(unit + length, all * heads);
-    if (unit >= last_unit) return;
+    const int mine = chunk_tiles(a, my_from, my_to);
+    const int upto = scan_threads(mine, scan);
+    const int all = uniform(scan[0] + scan[1] + scan[2] + scan[3]);
+    const int length = piece_length(all * heads);
+    const int64_t begin = (int64_t)blockIdx.x * length;
+    if (begin >= all * heads) return;
+    int unit = (int)begin;
+    const int last_unit = min(unit + length, all * heads);
     {
-        int64_t at = (upto - mine) * heads;
+        int at = (upto - mine) * heads;
         if (unit >= at && unit < upto * heads) {
             int s = my_from;
             for (;; ++s) {
-                const int64_t n = (int64_t)seq_work(a, s).tiles * heads;
+                const int n = seq_work(a, s).tiles * heads;
                 if (unit < at + n) break;
                 at += n;
             }
@@ -137,26 +135,32 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
         }
     }
     __syncthreads();
-    int s = __builtin_amdgcn_readfirstlane((int)found[0]);
-    int64_t seq_unit = found[1];   // first unit of sequence s
+    int s = uniform(found[0]);
+    int seq_unit = uniform(found[1]);   // first unit of sequence s
 
     char* const my_v = lds + wave * (kWaveKeys * D * 2);
+    const Widen<BITS> widen;
+    // scores are in units of log 2 where nothing but the scale is done to them
+    const float factor = SHAPED ? a.scale : a.scale * kLog2e;
+    // a lane's place in 16 rows of keys (a quarter of row `col`) and in VR rows of values
+    const uint32_t k_offset = col * (D * BITS / 8) + (BITS == 3 && D == 64 ? (6 * quarter) & ~3 : quarter * (KW * 4));
+    const uint32_t v_offset = (lane / VL) * (D * BITS / 8) + (BITS == 3 && D == 64 ? (6 * (lane % VL)) & ~3 : (lane % VL) * (VW * 4));
     const Partial part = partial_of(a.partial, 16 * NR, D);
 
     while (unit < last_unit) {
-        const SeqWork w = seq_work(a, s);
-        if (unit >= seq_unit + (int64_t)w.tiles * heads) {   // (sequences without tiles are passed over)
-            seq_unit += (int64_t)w.tiles * heads;
+        const SeqWork w = seq_work<true>(a, s);
+        if (unit >= seq_unit + w.tiles * heads) {   // (sequences without tiles are passed over)
+            seq_unit += w.tiles * heads;
             ++s;
             continue;
         }
-        const int in_seq = (int)(unit - seq_unit), head = in_seq / w.tiles;
+        const int in_seq = unit - seq_unit, head = in_seq / w.tiles;
         const int t0 = in_seq - head * w.tiles;
-        const int t1 = (int)min((int64_t)w.tiles, t0 + (last_unit - unit));
+        const int t1 = min(w.tiles, t0 + last_unit - unit);
         unit += t1 - t0;
         const int rows = w.rows_q * a.group;
         const int before = w.span.total - w.span.n;
-        const int prefix = a.prefix_lens ? a.prefix_lens[s] : 0;
+        const int prefix = a.prefix_lens ? table_entry(a.prefix_lens, s) : 0;
         const int32_t* table = a.batch.block_table + s * a.batch.table_stride;
 
         // queries: column `col` of row tile r is row 16 r + col of (token, query head of the group)
@@ -189,6 +193,21 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
             see[r] = visible_keys(position[r], w.span.keys, a.window, prefix);
             slope[r] = a.slopes && live ? a.slopes[h] : 0.0f;
         }
+        // keys that all rows see
+        int all_lo = 0, all_hi = 0x7FFFFFFF;
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+            if (16 * r + col < rows) {
+                all_lo = max(all_lo, see[r].lo);
+                all_hi = min(all_hi, see[r].hi);
+            }
+#pragma unroll
+        for (int x = 1; x < 16; x <<= 1) {
+            all_lo = max(all_lo, __shfl_xor(all_lo, x, 64));
+            all_hi = min(all_hi, __shfl_xor(all_hi, x, 64));
+        }
+        all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+        all_hi = __builtin_amdgcn_readfirstlane(all_hi);
         f32x4 o[NR][D / 16], psum[NR];
         float m[NR], l[NR];
 #pragma unroll
@@ -200,66 +219,66 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
             for (int i = 0; i < D / 16; ++i) o[r][i] = (f32x4){0, 0, 0, 0};
         }
 
-        // pages of the two groups of 16 keys of a tile (a page holds whole groups); -1 where none is to be read
-        auto page_of = [&](int key) {   // (beyond the end: the last key's entry is read, and not used)
-            const int p = table_entry(table, (key < w.end ? key : w.end - 1) >> a.cache.page_shift);
-            return key < w.end && (uint32_t)p < (uint32_t)a.cache.n_pages ? p : -1;
+        // Pages of the two groups of 16 keys of a tile (a page holds whole groups).  Loads go out unconditionally, so that their number
+        // between an operand's load and its use is known and a wait for it need not wait for those behind it: where there is no page
+        // (entry), or no key, some page's rows are read in place, and hidden.
+        struct Pages {
+            int entry[2];
         };
-        auto row_of = [&](int page, int key) {
-            return (int64_t)page * a.cache.page_rows + ((int64_t)head << a.cache.page_shift) + (key & page_mask);
+        const int last_key = w.base + (w.tiles - 1) * kTileKeys + wave * kWaveKeys;
+        auto pages_of = [&](int key) {
+            Pages p;
+            p.entry[0] = table_entry(table, min(key, w.end - 1) >> a.cache.page_shift);
+            p.entry[1] = a.cache.page_shift >= 5 ? p.entry[0] : table_entry(table, min(key + 16, w.end - 1) >> a.cache.page_shift);
+            return p;
         };
-        auto load_k = [&](int key0, const int* page, uint32_t (*k)[KW], f32x4* ks) {
+        auto there = [&](int page) { return (uint32_t)page < (uint32_t)a.cache.n_pages; };
+        auto row_of = [&](const Pages& p, int g, int key) {
+            return (int64_t)(there(p.entry[g]) ? p.entry[g] : 0) * a.cache.page_rows + ((int64_t)head << a.cache.page_shift) + (key & page_mask);
+        };
+        constexpr int ROW = D * BITS / 8;   // bytes
+        // A lane's quarter of a row of codes, or of keys in 16 bits.
+        auto load_row = [&](const uint8_t* at, int part, uint32_t* x) {
+            load_dwords<KW>(at, x);
+            if constexpr (BITS == 3 && D == 64) {   // six bytes, in two dwords from the one on that holds the first
+                if (part & 1) {
+                    x[0] = (x[0] >> 16) | (x[1] << 16);
+                    x[1] >>= 16;
+                }
+            }
+        };
+        auto load_k = [&](int key0, const Pages& p, uint32_t (*k)[KW], f32x4* ks) {
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
-                ks[g] = (f32x4){0, 0, 0, 0};
-#pragma unroll
-                for (int i = 0; i < KW; ++i) k[g][i] = 0;
-                if (page[g] < 0) continue;
-                const int key = key0 + 16 * g;
-                const int64_t row = row_of(page[g], key);
-                if (key + col < w.end) {
-                    const uint8_t* at = a.cache.k + (row + col) * (D * BITS / 8);
-                    if constexpr (BITS == 3 && D == 64) {   // six bytes, from the dword on that holds the first
-                        load_dwords<2>(at + ((6 * quarter) & ~3), k[g]);
-                        if (quarter & 1) {
-                            k[g][0] = (k[g][0] >> 16) | (k[g][1] << 16);
-                            k[g][1] >>= 16;
-                        }
-                    } else {
-                        load_dwords<KW>(at + quarter * (KW * 4), k[g]);
-                    }
-                }
+                const int64_t row = row_of(p, g, key0 + 16 * g);
+                load_row(a.cache.k + row * ROW + k_offset, quarter, k[g]);
                 if constexpr (BITS != 16) load_dwords<4>(a.cache.k_scales + row + 4 * quarter, reinterpret_cast<uint32_t*>(&ks[g]));
             }
         };
-
-        uint32_t k[2][KW];
-        f32x4 ks[2];
-        int key0 = w.base + t0 * kTileKeys + wave * kWaveKeys;
-        const int key_end = min(w.end, w.base + t1 * kTileKeys);
-        int page[2] = {page_of(key0), page_of(key0 + 16)};
-        int next_page[2] = {page_of(key0 + kTileKeys), page_of(key0 + kTileKeys + 16)};
-        load_k(key0, page, k, ks);
-        for (; key0 < key_end; key0 += kTileKeys) {
-            // values of this tile
-            uint32_t v[VS][VW];
-            f32x4 vs[2];
+        auto load_v = [&](int key0, const Pages& p, uint32_t (*v)[VW], f32x4* vs) {
 #pragma unroll
             for (int i = 0; i < VS; ++i) {
-                const int in_tile = i * VR + lane / VL;
-                const int pg = in_tile < 16 ? page[0] : page[1];
-#pragma unroll
-                for (int j = 0; j < VW; ++j) v[i][j] = 0;
-                if (pg >= 0 && key0 + in_tile < w.end)
-                    load_dwords<VW>(a.cache.v + row_of(pg, key0 + in_tile) * (D * BITS / 8) + (lane % VL) * (VW * 4), v[i]);
+                const uint8_t* at = a.cache.v + row_of(p, i * VR / 16, key0 + i * VR) * ROW + v_offset;
+                if constexpr (BITS == 16) load_dwords<VW>(at, v[i]);
+                else load_row(at, lane & 3, v[i]);
             }
             if constexpr (BITS != 16) {
 #pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    vs[g] = (f32x4){0, 0, 0, 0};
-                    if (page[g] >= 0) load_dwords<4>(a.cache.v_scales + row_of(page[g], key0 + 16 * g) + 4 * quarter, reinterpret_cast<uint32_t*>(&vs[g]));
-                }
+                for (int g = 0; g < 2; ++g)
+                    load_dwords<4>(a.cache.v_scales + row_of(p, g, key0 + 16 * g) + 4 * quarter, reinterpret_cast<uint32_t*>(&vs[g]));
             }
+        };
+
+        uint32_t k[2][KW], v[VS][VW];
+        f32x4 ks[2], vs[2];
+        int key0 = w.base + t0 * kTileKeys + wave * kWaveKeys;
+        const int key_end = w.base + t1 * kTileKeys;
+        Pages here = pages_of(key0), next = pages_of(min(key0 + kTileKeys, last_key));
+        load_k(key0, here, k, ks);
+        load_v(key0, here, v, vs);
+        for (; key0 < key_end; key0 += kTileKeys) {
+            const int next_key = min(key0 + kTileKeys, last_key);   // (the last tile is fetched twice: from a cache then)
+            const Pages after = pages_of(min(key0 + 2 * kTileKeys, last_key));
             // scores of two groups of 16 keys
             f32x4 score[NR][2];
 #pragma unroll
@@ -270,7 +289,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
             for (int g = 0; g < 2; ++g)
 #pragma unroll
                 for (int i = 0; i < G8; ++i) {
-                    const bf16x8 kk = __builtin_bit_cast(bf16x8, widen_codes<BITS>(k[g], i));
+                    const bf16x8 kk = __builtin_bit_cast(bf16x8, widen(k[g], i));
 #pragma unroll
                     for (int r = 0; r < NR; ++r) {
                         const bf16x8 qq = __builtin_bit_cast(bf16x8, (u32x4){q[r][4 * i], q[r][4 * i + 1], q[r][4 * i + 2], q[r][4 * i + 3]});
@@ -281,33 +300,28 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
 #pragma unroll
             for (int g = 0; g < 2; ++g) k_scale[g] = ks[g];
             // keys of the next tile
-            const int here[2] = {page[0], page[1]};
-            page[0] = next_page[0];
-            page[1] = next_page[1];
-            load_k(key0 + kTileKeys, page, k, ks);
-            next_page[0] = page_of(key0 + 2 * kTileKeys);
-            next_page[1] = page_of(key0 + 2 * kTileKeys + 16);
-
+            load_k(next_key, next, k, ks);
+            const bool open = key0 >= all_lo && key0 + kWaveKeys <= all_hi && there(here.entry[0]) && there(here.entry[1]);
             bf16x8 p[NR];
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
                 float x[8];
-                bool seen[8];
                 float top = -INFINITY;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int j = key0 + 16 * (i >> 2) + 4 * quarter + (i & 3);
-                    float y = score[r][i >> 2][i & 3];
-                    const float f = BITS == 16 ? a.scale : a.scale * k_scale[i >> 2][i & 3];
-                    if (a.softcap > 0.0f || a.slopes) {
-                        y = capped_score(y * f, a.softcap) - slope[r] * kLog2e * fabsf((float)(position[r] - j));
-                    } else {
-                        y *= f * kLog2e;
-                    }
-                    seen[i] = j >= see[r].lo && j < see[r].hi && here[i >> 2] >= 0;
-                    x[i] = seen[i] ? y : -INFINITY;
-                    top = fmaxf(top, x[i]);
+                    x[i] = score[r][i >> 2][i & 3] * (BITS == 16 ? factor : factor * k_scale[i >> 2][i & 3]);
+                    if constexpr (SHAPED) x[i] = capped_score(x[i], a.softcap) - slope[r] * kLog2e * fabsf((float)(position[r] - j));
                 }
+                if (!open) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int j = key0 + 16 * (i >> 2) + 4 * quarter + (i & 3);
+                        if (j < see[r].lo || j >= see[r].hi || !there(here.entry[i >> 2])) x[i] = -INFINITY;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
                 top = fmaxf(m[r], join16(join32(top, MaxOf()), MaxOf()));
                 if (__any(top > m[r])) {   // (rare after the first tiles)
                     const float keep = top > m[r] ? __builtin_amdgcn_exp2f(m[r] - top) : 1.0f;
@@ -324,46 +338,68 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
                 for (int i = 0; i < 8; ++i) {
                     const float e = __builtin_amdgcn_exp2f(x[i] - ref);
                     l[r] += e;
-                    weight[i] = BITS == 16 ? e : (seen[i] ? e * vs[i >> 2][i & 3] : 0.0f);
+                    weight[i] = BITS == 16 ? e : (open || e > 0.0f ? e * vs[i >> 2][i & 3] : 0.0f);   // (what is hidden may have any scale)
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) packed[i] = pack_bf16(weight[2 * i], weight[2 * i + 1]);
                 p[r] = __builtin_bit_cast(bf16x8, (u32x4){packed[0], packed[1], packed[2], packed[3]});
             }
 
-            // values through LDS: rows in, columns out
-            asm volatile("" ::: "memory");
+            // values through LDS: rows in, columns out.  (Hidden rows of 16 bits may hold anything: zeros.  Any code is a number.)
+            if (BITS == 16 && !open) {
 #pragma unroll
-            for (int i = 0; i < VS; ++i) {
-                const int in_tile = i * VR + lane / VL;
+                for (int i = 0; i < VS; ++i) {
+                    const bool keep = key0 + i * VR + lane / VL < w.end && there(here.entry[i * VR / 16]);
 #pragma unroll
-                for (int g = 0; g < VC / 8; ++g)
-                    *reinterpret_cast<u32x4*>(my_v + v_place<D>(in_tile, (lane % VL) * (VC / 8) + g)) = widen_codes<BITS>(v[i], g);
+                    for (int j = 0; j < VW; ++j) v[i][j] = keep ? v[i][j] : 0;
+                }
             }
             asm volatile("" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < VS; ++i)
+#pragma unroll
+                for (int g = 0; g < V8; ++g)
+                    *reinterpret_cast<u32x4*>(my_v + v_place<D>(i * VR + lane / VL, (lane % VL) * V8 + g)) = widen(v[i], g);
+            asm volatile("" ::: "memory");
+            // values of the next tile: like its keys they have the time of a tile to arrive
+            load_v(next_key, next, v, vs);
             if constexpr (BITS != 16) {
                 const bf16x8 ones = __builtin_bit_cast(bf16x8, (u32x4){0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
 #pragma unroll
                 for (int r = 0; r < NR; ++r) psum[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[r], psum[r], 0, 0, 0);
             }
+            // Four columns' tiles are read while four are multiplied.  (All at once, as the compiler would, they take the registers of a
+            // third wave.)
+            uint32_t columns[2][4][4];
+            auto read_columns = [&](int first, uint32_t (*to)[4]) {
 #pragma unroll
-            for (int i = 0; i < D / 16; ++i) {
-                // lane (16 b + c) supplies row 4 b + c / 4, features 4 (c mod 4) on, and gets feature c of rows 4 b to 4 b + 3
-                uint32_t col_v[4];
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const int row = 16 * g + 4 * quarter + (col >> 2);
-                    const int byte = v_place<D>(row, 2 * i + ((col & 3) >> 1)) + 8 * (col & 1);
-                    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-                    const s16x4 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(my_v + byte));
-                    const uint2 u = __builtin_bit_cast(uint2, c);
-                    col_v[2 * g] = u.x;
-                    col_v[2 * g + 1] = u.y;
+                    for (int g = 0; g < 2; ++g) {
+                        // lane (16 b + c) supplies row 4 b + c / 4, features 4 (c mod 4) on, and gets feature c of rows 4 b to 4 b + 3
+                        const int row = 16 * g + 4 * quarter + (col >> 2);
+                        const int byte = v_place<D>(row, 2 * (first + i) + ((col & 3) >> 1)) + 8 * (col & 1);
+                        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+                        const uint2 u = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(my_v + byte)));
+                        to[i][2 * g] = u.x;
+                        to[i][2 * g + 1] = u.y;
+                    }
+            };
+            read_columns(0, columns[0]);
+#pragma unroll
+            for (int f = 0; f < D / 16; f += 4) {
+                __builtin_amdgcn_sched_barrier(0);
+                if (f + 4 < D / 16) read_columns(f + 4, columns[(f / 4 + 1) & 1]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t* c = columns[(f / 4) & 1][i];
+                    const bf16x8 vv = __builtin_bit_cast(bf16x8, (u32x4){c[0], c[1], c[2], c[3]});
+#pragma unroll
+                    for (int r = 0; r < NR; ++r) o[r][f + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, p[r], o[r][f + i], 0, 0, 0);
                 }
-                const bf16x8 vv = __builtin_bit_cast(bf16x8, (u32x4){col_v[0], col_v[1], col_v[2], col_v[3]});
-#pragma unroll
-                for (int r = 0; r < NR; ++r) o[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, p[r], o[r][i], 0, 0, 0);
             }
+            here = next;
+            next = after;
         }
 
         // the four waves' results joined, 16 rows at a time
@@ -372,7 +408,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
         const bool whole = t0 == 0 && t1 == w.tiles;
         if (t0 == 0 && threadIdx.x == 0)   // (unit is the end of this piece: what is left of the tiles follows, `length` a workgroup)
             held_by(a.partial, 16 * NR, D)[s * heads + head] =
-                make_int2((int)blockIdx.x, (int)blockIdx.x + (int)((w.tiles - t1 + length - 1) / length));
+                make_int2((int)blockIdx.x, (int)blockIdx.x + (w.tiles - t1 + length - 1) / length);
         const int slot = 2 * (int)blockIdx.x + (t0 == 0);
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
@@ -428,7 +464,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
 // Joins the partial results of one (sequence, key head) a workgroup; zeros where there was nothing to see.
 __global__ __launch_bounds__(kThreads) void paged_decode_join_kernel(AttentionArgs a, int tile_rows) {
     const int heads = a.cache.heads, s = blockIdx.x / heads, head = blockIdx.x - s * heads;
-    const SeqWork w = seq_work(a, s);
+    const SeqWork w = seq_work<true>(a, s);
     const int2 held = held_by(a.partial, tile_rows, a.d)[blockIdx.x];   // (nobody notes anything where there are no tiles)
     const int g0 = w.tiles > 0 ? held.x : 0, g1 = w.tiles > 0 ? held.y : -1;
     if (g0 == g1) return;   // one workgroup had it all
@@ -456,18 +492,20 @@ __global__ __launch_bounds__(kThreads) void paged_decode_join_kernel(AttentionAr
     }
 }
 
-template <int D, int BITS, int NR>
+template <int D, int BITS, int NR, bool SHAPED>
 int launch_form(const AttentionArgs& a, hipStream_t stream) {
     constexpr size_t lds = decode_lds(D);
-    if (int rc = allow_dynamic_lds<&paged_decode_kernel<D, BITS, NR>, lds>(); rc != HBL_OK) return rc;
-    launch_kernel("paged_decode_kernel", paged_decode_kernel<D, BITS, NR>, dim3(kPieces), dim3(kThreads), lds, stream, a);
+    if (int rc = allow_dynamic_lds<&paged_decode_kernel<D, BITS, NR, SHAPED>, lds>(); rc != HBL_OK) return rc;
+    launch_kernel("paged_decode_kernel", paged_decode_kernel<D, BITS, NR, SHAPED>, dim3(kPieces), dim3(kThreads), lds, stream, a);
     launch_kernel("paged_decode_join_kernel", paged_decode_join_kernel, dim3((unsigned)a.batch.n_seqs * (unsigned)a.cache.heads), dim3(kThreads), 0,
                   stream, a, 16 * NR);
     return after_launch();
 }
 template <int D, int BITS>
 int launch_rows(const AttentionArgs& a, hipStream_t stream) {
-    return a.max_q * a.group <= 16 ? launch_form<D, BITS, 1>(a, stream) : launch_form<D, BITS, 2>(a, stream);
+    const bool shaped = a.softcap > 0.0f || a.slopes;
+    if (a.max_q * a.group <= 16) return shaped ? launch_form<D, BITS, 1, true>(a, stream) : launch_form<D, BITS, 1, false>(a, stream);
+    return shaped ? launch_form<D, BITS, 2, true>(a, stream) : launch_form<D, BITS, 2, false>(a, stream);
 }
 template <int D>
 int launch_bits(const AttentionArgs& a, int bits, hipStream_t stream) {

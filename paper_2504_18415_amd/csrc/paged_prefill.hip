@@ -35,8 +35,9 @@ struct Item {
     SeqSpan span;
     int rows;      // of the sequence (tokens looked at times group)
 };
+template <bool UNIFORM = false>
 __device__ __forceinline__ Item item_of(const AttentionArgs& a, int s, int tile) {
-    Item it{s, tile, span_of(a.batch, a.cache.page_shift, a.T, s), 0};
+    Item it{s, tile, UNIFORM ? uniform_span(a.batch, a.T, s) : span_of(a.batch, a.T, s), 0};
     it.rows = (it.span.n < a.max_q ? it.span.n : a.max_q) * a.group;
     return it;
 }
@@ -146,6 +147,7 @@ __device__ __forceinline__ Unit find_unit(const AttentionArgs& a, Search* lds, i
         if (w < wave) at += lds->sums[w];
         unit.all += lds->sums[w];
     }
+    unit.all = uniform(unit.all);
     const int rank = rank_of(unit.all);
     for (int s = from; s < to; ++s) {
         const int parts = parts_of(s), n = row_tiles(a, s) * parts;
@@ -225,8 +227,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
                                            ? Done{unit.s, unit.tile, head, rank * heads + head, unit.parts}
                                            : Done{-1, 0, 0, 0, 0};
     if (!mine_at_all) return;
-    const Item it = item_of(a, unit.s, unit.tile);
-    const int prefix = a.prefix_lens ? a.prefix_lens[it.s] : 0;
+    const Item it = item_of<true>(a, unit.s, unit.tile);
+    const int prefix = a.prefix_lens ? table_entry(a.prefix_lens, it.s) : 0;
     const TileKeys keys = tile_keys(a, it, prefix, TK);
     const Part mine = part_of((keys.end - keys.base + TK - 1) / TK, unit.part, unit.parts);
     const int32_t* table = a.batch.block_table + it.s * a.batch.table_stride;
@@ -351,6 +353,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
     // codes: a chunk of keys and one of values a thread (D = 64: the first half of the threads keys, the second values)
     constexpr bool BOTH = CHUNKS == kThreads;
     const int chunk = BOTH ? threadIdx.x : threadIdx.x % CHUNKS, chunk_row = chunk / CR, chunk_at = chunk % CR;
+    const Widen<BITS> widen;
     uint32_t raw[2][CW];
     float raw_scale = 0.0f;
     auto fetch_codes = [&](int key0) {
@@ -377,7 +380,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int place = values ? v_place<D>(chunk_row, 4 * chunk_at + g) : k_place<D>(chunk_row, 4 * chunk_at + g);
-                *reinterpret_cast<u32x4*>(side(buffer, values) + place) = widen_codes<BITS>(raw[which], g);
+                *reinterpret_cast<u32x4*>(side(buffer, values) + place) = widen(raw[which], g);
             }
         }
         if ((int)threadIdx.x < 2 * TK) scales[buffer * 2 * TK + threadIdx.x] = raw_scale;
@@ -569,14 +572,12 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
 }
 
 // Joins the parts of a quarter of a row tile (32 rows) of a key head a workgroup.
-__global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(AttentionArgs a, int tile, int most) {
+__global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(AttentionArgs a, int most) {
     const int quarter = blockIdx.x & 3, heads = a.cache.heads;
     const Done unit = done_of(a, most)[blockIdx.x >> 2];
     if (unit.s < 0) return;
     const int head = unit.head;
-    const Item it = item_of(a, unit.s, unit.tile);
-    const TileKeys keys = tile_keys(a, it, a.prefix_lens ? a.prefix_lens[it.s] : 0, tile);
-    const int tiles = (keys.end - keys.base + tile - 1) / tile;
+    const Item it = item_of<true>(a, uniform(unit.s), unit.tile);
     const float2* const part_ml = reinterpret_cast<const float2*>(a.partial + (size_t)most * kRows * a.d);
     const int rows = min(32, it.rows - it.tile * kRows - 32 * quarter);
     for (int i = threadIdx.x; i < rows * (a.d / 4); i += kThreads) {
@@ -584,14 +585,13 @@ __global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(AttentionA
         const int token = row / a.group, h = head * a.group + row - token * a.group;
         float top = -INFINITY, total = 0.0f;
         f32x4 y = {0, 0, 0, 0};
-        for (int x = 0; x < unit.parts; ++x) {
-            const Part p = part_of(tiles, x, unit.parts);
-            if (p.from == p.to) continue;
+#pragma unroll 4
+        for (int x = 0; x < unit.parts; ++x) {   // (a part without keys has left -inf, 0 and zeros)
             const size_t at_row = ((size_t)unit.slot + (size_t)x * heads) * kRows + r;
             const float2 ml = part_ml[at_row];
             const f32x4 o = *reinterpret_cast<const f32x4*>(a.partial + at_row * a.d + at);
-            if (ml.x == -INFINITY) continue;
-            const float to = fmaxf(top, ml.x), keep = __builtin_amdgcn_exp2f(top - to), f = __builtin_amdgcn_exp2f(ml.x - to);
+            const float to = fmaxf(top, ml.x), ref = to == -INFINITY ? 0.0f : to;
+            const float keep = __builtin_amdgcn_exp2f(top - ref), f = __builtin_amdgcn_exp2f(ml.x - ref);
             total = total * keep + f * ml.y;
             y = y * keep + f * o;
             top = to;
@@ -641,7 +641,7 @@ int launch_form(const AttentionArgs& a, hipStream_t stream) {
     else rc = launch_shape<D, BITS, kScaled>(a, (unsigned)wgs, round, most, stream);
     if (rc != HBL_OK) return rc;
     if (cut)
-        launch_kernel("paged_prefill_join_kernel", paged_prefill_join_kernel, dim3((unsigned)(4 * wgs)), dim3(kThreads), 0, stream, a, kTile<D>, most);
+        launch_kernel("paged_prefill_join_kernel", paged_prefill_join_kernel, dim3((unsigned)(4 * wgs)), dim3(kThreads), 0, stream, a, most);
     return after_launch();
 }
 template <int D>

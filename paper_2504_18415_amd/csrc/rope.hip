@@ -226,7 +226,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a) {
     const int t = blockIdx.x;
     const int s = sequence_of(a.batch, t);
     if (s < 0) return;   // (before the first sequence, or ...
-    const SeqSpan span = span_of(a.batch, a.cache.page_shift, a.T, s);
+    const SeqSpan span = span_of(a.batch, a.T, s);
     const int in_seq = t - span.first;
     if (in_seq >= span.n) return;   // ... behind its end: left as it was)
     const int position = span.total - span.n + in_seq;

@@ -663,7 +663,7 @@ int hbl_kv_append(const hbl_kv_cache* cache, const hbl_kv_batch* batch, const vo
 size_t hbl_paged_attention_workspace_bytes(const hbl_kv_cache* cache, const hbl_kv_batch* batch, int64_t T, int64_t n_q_heads,
                                            int64_t max_q_len) {
     if (check_attention_shape(cache, batch, T, n_q_heads, max_q_len) != HBL_OK) return 0;
-    return paged_attention_workspace(T, batch->n_seqs, (int)n_q_heads, cache->n_kv_heads, cache->d, max_q_len < T ? max_q_len : T);
+    return paged_attention_workspace(T, batch->n_seqs, (int)n_q_heads, cache->n_kv_heads, cache->d, cache->bits, max_q_len < T ? max_q_len : T);
 }
 
 int hbl_paged_attention(const void* q, int64_t T, int64_t n_q_heads, int64_t q_stride, const hbl_kv_cache* cache,

@@ -34,12 +34,12 @@ struct AttentionArgs {
 };
 
 // Bytes of workspace of a call (T tokens, n_seqs sequences, Hq / Hkv heads of d).
-size_t paged_attention_workspace(int64_t T, int n_seqs, int Hq, int Hkv, int d, int64_t max_q_len);
+size_t paged_attention_workspace(int64_t T, int n_seqs, int Hq, int Hkv, int d, int bits, int64_t max_q_len);
 int launch_paged_attention(const AttentionArgs& a, int bits, void* workspace, hipStream_t stream);
 
 // Few rows a key head (paged_decode.hip): at most kDecodeRows tokens times query heads of a group.
 constexpr int kDecodeRows = 32;
-size_t paged_decode_workspace(int rows, int d, int n_seqs, int heads);
+size_t paged_decode_workspace(int rows, int d, int bits, int n_seqs, int heads);
 int launch_paged_decode(const AttentionArgs& a, int bits, hipStream_t stream);
 
 // More rows (paged_prefill.hip).

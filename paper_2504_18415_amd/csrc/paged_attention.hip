@@ -4,9 +4,9 @@
 
 namespace hbl {
 
-size_t paged_attention_workspace(int64_t T, int n_seqs, int Hq, int Hkv, int d, int64_t max_q_len) {
+size_t paged_attention_workspace(int64_t T, int n_seqs, int Hq, int Hkv, int d, int bits, int64_t max_q_len) {
     const int64_t rows = max_q_len * (Hq / Hkv);
-    const size_t bytes = rows <= kDecodeRows ? paged_decode_workspace((int)rows, d, n_seqs, Hkv) : paged_prefill_workspace(T, n_seqs, Hq / Hkv, Hkv, d);
+    const size_t bytes = rows <= kDecodeRows ? paged_decode_workspace((int)rows, d, bits, n_seqs, Hkv) : paged_prefill_workspace(T, n_seqs, Hq / Hkv, Hkv, d);
     return round_up(bytes > 0 ? bytes : 1, 256);
 }
 

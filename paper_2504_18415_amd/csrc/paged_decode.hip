@@ -15,7 +15,14 @@ namespace hbl {
 namespace {
 
 constexpr int kWaves = 4, kWaveKeys = 32, kTileKeys = kWaves * kWaveKeys, kThreads = 64 * kWaves;
-constexpr int kPieces = 512;   // workgroups: two for each of the 256 CUs
+// Workgroups of a launch: as many as the 256 CUs hold at once (by registers), of 16-bit heads of 64 two a CU.  (64 sequences of 8000
+// keys, heads of 128, 4 bits: 512 82 us, 768 77, 1024 91; heads of 256, 4 bits: 256 59 us, 512 69; heads of 64, 4 bits: 512 63 us,
+// 1024 54; 16 bits: 512 68 us, 1024 69.)
+constexpr int pieces_of(int d, int bits, int row_tiles) {
+    if (d == 256) return 256;
+    if (row_tiles == 2) return 512;
+    return bits <= 4 ? (d == 64 ? 1024 : 768) : bits == 8 && d == 64 ? 768 : 512;
+}
 
 // Keys that some row of a sequence sees, from a multiple of 32 on, and their tiles.
 struct SeqWork {
@@ -53,7 +60,7 @@ __device__ __forceinline__ int chunk_tiles(const AttentionArgs& a, int from, int
 }
 
 // The line of tiles cut into equal pieces.
-__device__ __forceinline__ int piece_length(int all_units) { return all_units < 1 ? 1 : (all_units + kPieces - 1) / kPieces; }
+__device__ __forceinline__ int piece_length(int all_units, int pieces) { return all_units < 1 ? 1 : (all_units + pieces - 1) / pieces; }
 
 // Inclusive sum over the workgroup's threads.
 __device__ __forceinline__ int scan_threads(int v, int* lds) {
@@ -80,11 +87,11 @@ struct Partial {
     float* o;
     float2* ml;
 };
-__device__ __forceinline__ Partial partial_of(float* base, int rows, int d) {
-    return {base, reinterpret_cast<float2*>(base + (size_t)2 * kPieces * rows * d)};
+__device__ __forceinline__ Partial partial_of(float* base, int pieces, int rows, int d) {
+    return {base, reinterpret_cast<float2*>(base + (size_t)2 * pieces * rows * d)};
 }
-__device__ __forceinline__ int2* held_by(float* base, int rows, int d) {
-    return reinterpret_cast<int2*>(base + (size_t)2 * kPieces * rows * (d + 2));
+__device__ __forceinline__ int2* held_by(float* base, int pieces, int rows, int d) {
+    return reinterpret_cast<int2*>(base + (size_t)2 * pieces * rows * (d + 2));
 }
 
 // Byte position of a 16-byte chunk in a wave's values in LDS.  Chunks are moved about by row so that the eight rows of which a
@@ -111,32 +118,47 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
     const int heads = a.cache.heads, page_mask = (1 << a.cache.page_shift) - 1;
 
     // my piece of the line
-    const int per_thread = (a.batch.n_seqs + kThreads - 1) / kThreads;
-    const int my_from = min((int)threadIdx.x * per_thread, a.batch.n_seqs), my_to = min(my_from + per_thread, a.batch.n_seqs);
-    const int mine = chunk_tiles(a, my_from, my_to);
-    const int upto = scan_threads(mine, scan);
-    const int all = uniform(scan[0] + scan[1] + scan[2] + scan[3]);
-    const int length = piece_length(all * heads);
-    const int64_t begin = (int64_t)blockIdx.x * length;
-    if (begin >= all * heads) return;
-    int unit = (int)begin;
-    const int last_unit = min(unit + length, all * heads);
-    {
+    constexpr int kPieces = pieces_of(D, BITS, NR);
+    int s, seq_unit, unit, last_unit, length;   // sequence and its first unit; my units; those of every workgroup
+    if (a.batch.n_seqs <= 64) {   // a sequence a lane, each wave for itself
+        const int mine = lane < a.batch.n_seqs ? seq_work(a, lane).tiles : 0;
+        int upto = mine;
+        for (int m = 1; m < a.batch.n_seqs; m <<= 1) {
+            const int u = __shfl_up(upto, m, 64);
+            if (lane >= m) upto += u;
+        }
+        const int all = __builtin_amdgcn_readlane(upto, a.batch.n_seqs - 1) * heads;
+        length = piece_length(all, kPieces);
+        if ((int64_t)blockIdx.x * length >= all) return;
+        unit = (int)blockIdx.x * length;
+        last_unit = min(unit + length, all);
+        s = __builtin_ctzll(__ballot(upto * heads > unit));
+        seq_unit = __builtin_amdgcn_readlane(upto - mine, s) * heads;
+    } else {
+        const int per_thread = (a.batch.n_seqs + kThreads - 1) / kThreads;
+        const int my_from = min((int)threadIdx.x * per_thread, a.batch.n_seqs), my_to = min(my_from + per_thread, a.batch.n_seqs);
+        const int mine = chunk_tiles(a, my_from, my_to);
+        const int upto = scan_threads(mine, scan);
+        const int all = uniform(scan[0] + scan[1] + scan[2] + scan[3]) * heads;
+        length = piece_length(all, kPieces);
+        if ((int64_t)blockIdx.x * length >= all) return;
+        unit = (int)blockIdx.x * length;
+        last_unit = min(unit + length, all);
         int at = (upto - mine) * heads;
         if (unit >= at && unit < upto * heads) {
-            int s = my_from;
-            for (;; ++s) {
-                const int n = seq_work(a, s).tiles * heads;
+            int i = my_from;
+            for (;; ++i) {
+                const int n = seq_work(a, i).tiles * heads;
                 if (unit < at + n) break;
                 at += n;
             }
-            found[0] = s;
+            found[0] = i;
             found[1] = at;
         }
+        __syncthreads();
+        s = uniform(found[0]);
+        seq_unit = uniform(found[1]);
     }
-    __syncthreads();
-    int s = uniform(found[0]);
-    int seq_unit = uniform(found[1]);   // first unit of sequence s
 
     char* const my_v = lds + wave * (kWaveKeys * D * 2);
     const Widen<BITS> widen;
@@ -145,7 +167,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
     // a lane's place in 16 rows of keys (a quarter of row `col`) and in VR rows of values
     const uint32_t k_offset = col * (D * BITS / 8) + (BITS == 3 && D == 64 ? (6 * quarter) & ~3 : quarter * (KW * 4));
     const uint32_t v_offset = (lane / VL) * (D * BITS / 8) + (BITS == 3 && D == 64 ? (6 * (lane % VL)) & ~3 : (lane % VL) * (VW * 4));
-    const Partial part = partial_of(a.partial, 16 * NR, D);
+    const Partial part = partial_of(a.partial, kPieces, 16 * NR, D);
 
     while (unit < last_unit) {
         const SeqWork w = seq_work<true>(a, s);
@@ -407,7 +429,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
         float* const join_ml = join_o + kWaves * 16 * merge_stride(D);
         const bool whole = t0 == 0 && t1 == w.tiles;
         if (t0 == 0 && threadIdx.x == 0)   // (unit is the end of this piece: what is left of the tiles follows, `length` a workgroup)
-            held_by(a.partial, 16 * NR, D)[s * heads + head] =
+            held_by(a.partial, kPieces, 16 * NR, D)[s * heads + head] =
                 make_int2((int)blockIdx.x, (int)blockIdx.x + (w.tiles - t1 + length - 1) / length);
         const int slot = 2 * (int)blockIdx.x + (t0 == 0);
 #pragma unroll
@@ -462,14 +484,14 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
 }
 
 // Joins the partial results of one (sequence, key head) a workgroup; zeros where there was nothing to see.
-__global__ __launch_bounds__(kThreads) void paged_decode_join_kernel(AttentionArgs a, int tile_rows) {
+__global__ __launch_bounds__(kThreads) void paged_decode_join_kernel(AttentionArgs a, int pieces, int tile_rows) {
     const int heads = a.cache.heads, s = blockIdx.x / heads, head = blockIdx.x - s * heads;
     const SeqWork w = seq_work<true>(a, s);
-    const int2 held = held_by(a.partial, tile_rows, a.d)[blockIdx.x];   // (nobody notes anything where there are no tiles)
+    const int2 held = held_by(a.partial, pieces, tile_rows, a.d)[blockIdx.x];   // (nobody notes anything where there are no tiles)
     const int g0 = w.tiles > 0 ? held.x : 0, g1 = w.tiles > 0 ? held.y : -1;
     if (g0 == g1) return;   // one workgroup had it all
     const int rows = w.rows_q * a.group;
-    const Partial part = partial_of(a.partial, tile_rows, a.d);
+    const Partial part = partial_of(a.partial, pieces, tile_rows, a.d);
     for (int i = threadIdx.x; i < rows * (a.d / 4); i += kThreads) {
         const int row = i / (a.d / 4), at = 4 * (i - row * (a.d / 4));
         const int token = row / a.group, h = head * a.group + row - token * a.group;
@@ -495,10 +517,11 @@ __global__ __launch_bounds__(kThreads) void paged_decode_join_kernel(AttentionAr
 template <int D, int BITS, int NR, bool SHAPED>
 int launch_form(const AttentionArgs& a, hipStream_t stream) {
     constexpr size_t lds = decode_lds(D);
+    constexpr int pieces = pieces_of(D, BITS, NR);
     if (int rc = allow_dynamic_lds<&paged_decode_kernel<D, BITS, NR, SHAPED>, lds>(); rc != HBL_OK) return rc;
-    launch_kernel("paged_decode_kernel", paged_decode_kernel<D, BITS, NR, SHAPED>, dim3(kPieces), dim3(kThreads), lds, stream, a);
+    launch_kernel("paged_decode_kernel", paged_decode_kernel<D, BITS, NR, SHAPED>, dim3(pieces), dim3(kThreads), lds, stream, a);
     launch_kernel("paged_decode_join_kernel", paged_decode_join_kernel, dim3((unsigned)a.batch.n_seqs * (unsigned)a.cache.heads), dim3(kThreads), 0,
-                  stream, a, 16 * NR);
+                  stream, a, pieces, 16 * NR);
     return after_launch();
 }
 template <int D, int BITS>
@@ -519,9 +542,9 @@ int launch_bits(const AttentionArgs& a, int bits, hipStream_t stream) {
 
 }  // namespace
 
-size_t paged_decode_workspace(int rows, int d, int n_seqs, int heads) {
+size_t paged_decode_workspace(int rows, int d, int bits, int n_seqs, int heads) {
     const int tile_rows = rows <= 16 ? 16 : 32;
-    return (size_t)2 * kPieces * tile_rows * (d + 2) * sizeof(float) + (size_t)n_seqs * heads * sizeof(int2);
+    return (size_t)2 * pieces_of(d, bits, tile_rows / 16) * tile_rows * (d + 2) * sizeof(float) + (size_t)n_seqs * heads * sizeof(int2);
 }
 
 int launch_paged_decode(const AttentionArgs& a, int bits, hipStream_t stream) {

@@ -185,62 +185,6 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
         const int prefix = a.prefix_lens ? table_entry(a.prefix_lens, s) : 0;
         const int32_t* table = a.batch.block_table + s * a.batch.table_stride;
 
-        // queries: column `col` of row tile r is row 16 r + col of (token, query head of the group)
-        uint32_t q[NR][QW];
-        float start[NR], slope[NR];
-        int position[NR];
-        KeyRange see[NR];
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            const int row = 16 * r + col, token = row / a.group, h = head * a.group + row - token * a.group;
-            const bool live = row < rows;
-            float sum = 0.0f;
-#pragma unroll
-            for (int g = 0; g < G8; ++g) {
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (live)
-                    x = *reinterpret_cast<const uint4*>(a.q + (w.span.first + token) * a.q_stride + (int64_t)h * D + quarter * (D / 4) + 8 * g);
-                const uint32_t y[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    // (feature i and i + 4 of the eight, or as they lie)
-                    q[r][4 * g + i] = !Codes<BITS>::kPaired ? y[i]
-                                                            : __builtin_amdgcn_perm(y[2 + (i >> 1)], y[i >> 1], (i & 1) ? 0x07060302u : 0x05040100u);
-                    sum += as_f(y[i] << 16) + as_f(y[i] & 0xFFFF0000u);
-                }
-            }
-            sum = join16(join32(sum, SumOf()), SumOf());
-            start[r] = -kBias * sum;
-            position[r] = live ? before + token : -1;
-            see[r] = visible_keys(position[r], w.span.keys, a.window, prefix);
-            slope[r] = a.slopes && live ? a.slopes[h] : 0.0f;
-        }
-        // keys that all rows see
-        int all_lo = 0, all_hi = 0x7FFFFFFF;
-#pragma unroll
-        for (int r = 0; r < NR; ++r)
-            if (16 * r + col < rows) {
-                all_lo = max(all_lo, see[r].lo);
-                all_hi = min(all_hi, see[r].hi);
-            }
-#pragma unroll
-        for (int x = 1; x < 16; x <<= 1) {
-            all_lo = max(all_lo, __shfl_xor(all_lo, x, 64));
-            all_hi = min(all_hi, __shfl_xor(all_hi, x, 64));
-        }
-        all_lo = __builtin_amdgcn_readfirstlane(all_lo);
-        all_hi = __builtin_amdgcn_readfirstlane(all_hi);
-        f32x4 o[NR][D / 16], psum[NR];
-        float m[NR], l[NR];
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            m[r] = -INFINITY;
-            l[r] = 0.0f;
-            psum[r] = (f32x4){0, 0, 0, 0};
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) o[r][i] = (f32x4){0, 0, 0, 0};
-        }
-
         // Pages of the two groups of 16 keys of a tile (a page holds whole groups).  Loads go out unconditionally, so that their number
         // between an operand's load and its use is known and a wait for it need not wait for those behind it: where there is no page
         // (entry), or no key, some page's rows are read in place, and hidden.
@@ -298,6 +242,51 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
         Pages here = pages_of(key0), next = pages_of(min(key0 + kTileKeys, last_key));
         load_k(key0, here, k, ks);
         load_v(key0, here, v, vs);
+        // (the first tile is on its way while these are fetched)
+        // queries: column `col` of row tile r is row 16 r + col of (token, query head of the group)
+        uint32_t q[NR][QW];
+        float start[NR], slope[NR];
+        int position[NR];
+        KeyRange see[NR];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            const int row = 16 * r + col, token = row / a.group, h = head * a.group + row - token * a.group;
+            const bool live = row < rows;
+            float sum = 0.0f;
+#pragma unroll
+            for (int g = 0; g < G8; ++g) {
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (live)
+                    x = *reinterpret_cast<const uint4*>(a.q + (w.span.first + token) * a.q_stride + (int64_t)h * D + quarter * (D / 4) + 8 * g);
+                const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    // (feature i and i + 4 of the eight, or as they lie)
+                    q[r][4 * g + i] = !Codes<BITS>::kPaired ? y[i]
+                                                            : __builtin_amdgcn_perm(y[2 + (i >> 1)], y[i >> 1], (i & 1) ? 0x07060302u : 0x05040100u);
+                    sum += as_f(y[i] << 16) + as_f(y[i] & 0xFFFF0000u);
+                }
+            }
+            sum = join16(join32(sum, SumOf()), SumOf());
+            start[r] = -kBias * sum;
+            position[r] = live ? before + token : -1;
+            see[r] = visible_keys(position[r], w.span.keys, a.window, prefix);
+            slope[r] = a.slopes && live ? a.slopes[h] : 0.0f;
+        }
+        // keys that all rows see: from where the last token begins to where the first one ends
+        const int all_lo = visible_keys(before + w.rows_q - 1, w.span.keys, a.window, prefix).lo;
+        const int all_hi = visible_keys(before, w.span.keys, a.window, prefix).hi;
+        f32x4 o[NR][D / 16], psum[NR];
+        float m[NR], l[NR];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            m[r] = -INFINITY;
+            l[r] = 0.0f;
+            psum[r] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) o[r][i] = (f32x4){0, 0, 0, 0};
+        }
+
         for (; key0 < key_end; key0 += kTileKeys) {
             const int next_key = min(key0 + kTileKeys, last_key);   // (the last tile is fetched twice: from a cache then)
             const Pages after = pages_of(min(key0 + 2 * kTileKeys, last_key));

@@ -28,7 +28,7 @@ constexpr int pieces_of(int d, int bits, int row_tiles) {
 struct SeqWork {
     SeqSpan span;
     int rows_q;       // tokens looked at
-    int base, end;    // keys
+    int base, lo, end;   // keys: a multiple of 32, the first, behind the last
     int tiles;
 };
 template <bool UNIFORM = false>
@@ -36,7 +36,7 @@ __device__ __forceinline__ SeqWork seq_work(const AttentionArgs& a, int s) {
     SeqWork w;
     w.span = UNIFORM ? uniform_span(a.batch, a.T, s) : span_of(a.batch, a.T, s);
     w.rows_q = w.span.n < a.max_q ? w.span.n : a.max_q;
-    w.base = w.end = w.tiles = 0;
+    w.base = w.lo = w.end = w.tiles = 0;
     const int before = w.span.total - w.span.n;   // position of the first token
     const int first = before < 0 ? -before : 0;   // the first one that has a place
     if (first < w.rows_q) {
@@ -45,6 +45,7 @@ __device__ __forceinline__ SeqWork seq_work(const AttentionArgs& a, int s) {
         const KeyRange hi = visible_keys(before + w.rows_q - 1, w.span.keys, a.window, prefix);
         if (hi.hi > lo.lo) {
             w.base = lo.lo & ~(kWaveKeys - 1);
+            w.lo = lo.lo;
             w.end = hi.hi;
             w.tiles = (w.end - w.base + kTileKeys - 1) / kTileKeys;
         }
@@ -313,6 +314,13 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
             // keys of the next tile
             load_k(next_key, next, k, ks);
             const bool open = key0 >= all_lo && key0 + kWaveKeys <= all_hi && there(here.entry[0]) && there(here.entry[1]);
+            if (BITS != 16 && !open) {   // what no row sees may have any scale: 0
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int j = key0 + 16 * (i >> 2) + 4 * quarter + (i & 3);
+                    if (j < w.lo || j >= w.end || !there(here.entry[i >> 2])) vs[i >> 2][i & 3] = 0.0f;
+                }
+            }
             bf16x8 p[NR];
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
@@ -349,7 +357,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
                 for (int i = 0; i < 8; ++i) {
                     const float e = __builtin_amdgcn_exp2f(x[i] - ref);
                     l[r] += e;
-                    weight[i] = BITS == 16 ? e : (open || e > 0.0f ? e * vs[i >> 2][i & 3] : 0.0f);   // (what is hidden may have any scale)
+                    weight[i] = BITS == 16 ? e : e * vs[i >> 2][i & 3];
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) packed[i] = pack_bf16(weight[2 * i], weight[2 * i + 1]);
@@ -360,7 +368,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
             if (BITS == 16 && !open) {
 #pragma unroll
                 for (int i = 0; i < VS; ++i) {
-                    const bool keep = key0 + i * VR + lane / VL < w.end && there(here.entry[i * VR / 16]);
+                    const int j = key0 + i * VR + lane / VL;
+                    const bool keep = j >= w.lo && j < w.end && there(here.entry[i * VR / 16]);
 #pragma unroll
                     for (int j = 0; j < VW; ++j) v[i][j] = keep ? v[i][j] : 0;
                 }

@@ -45,18 +45,18 @@ __device__ __forceinline__ int row_tiles(const AttentionArgs& a, int s) { return
 
 // Keys that some row of the tile sees, from a multiple of the tile of keys on.
 struct TileKeys {
-    int base, end;
+    int base, lo, end;   // a multiple of the tile of keys; the first key; behind the last
 };
 __device__ __forceinline__ TileKeys tile_keys(const AttentionArgs& a, const Item& it, int prefix, int tile) {
     const int before = it.span.total - it.span.n;
     int first = it.tile * kRows / a.group;
     const int last = min((it.tile + 1) * kRows, it.rows) - 1;
     if (first < -before) first = -before;
-    if (first > last / a.group) return {0, 0};
+    if (first > last / a.group) return {0, 0, 0};
     const KeyRange lo = visible_keys(before + first, it.span.keys, a.window, prefix);
     const KeyRange hi = visible_keys(before + last / a.group, it.span.keys, a.window, prefix);
-    if (hi.hi <= lo.lo) return {0, 0};
-    return {lo.lo & ~(tile - 1), hi.hi};
+    if (hi.hi <= lo.lo) return {0, 0, 0};
+    return {lo.lo & ~(tile - 1), lo.lo, hi.hi};
 }
 // How the work is cut: a unit is a row tile and a part of its keys.  All row tiles of a sequence have the same number of parts,
 // their keys over `length` tiles, rounded up.
@@ -85,7 +85,7 @@ __device__ __forceinline__ Unit find_unit(const AttentionArgs& a, Search* lds, i
     if (round > 0) {
         if ((int)threadIdx.x < n_seqs) {
             const int n = row_tiles(a, threadIdx.x);
-            TileKeys k{0, 0};
+            TileKeys k{0, 0, 0};
             if (n > 0) k = tile_keys(a, item_of(a, threadIdx.x, n - 1), a.prefix_lens ? a.prefix_lens[threadIdx.x] : 0, tile);
             lds->tiles[threadIdx.x] = n;
             lds->keys[threadIdx.x] = (k.end - k.base + tile - 1) / tile;
@@ -191,7 +191,7 @@ constexpr int kScaled = 0, kCapped = 1, kBiased = 2, kShaped = 3;
 constexpr float kLowCap = 40.0f;   // e^40 < 2^58, and e^-40 times a scale of 10^-20 is a normal number still
 
 template <int D, int BITS, int SHAPE>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kernel(AttentionArgs a, int round, int most) {
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void paged_prefill_kernel(AttentionArgs a, int round, int most) {
     constexpr int TK = kTile<D>, KB = TK / 32;              // blocks of 32 keys
     constexpr int RW = TK / kWaves;                         // rows of a tile that a wave loads (16 bits)
     constexpr int RI = 512 / D, NI = RW / RI;               // rows a load, loads
@@ -286,33 +286,24 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
     for (int i = 0; i < D / 32; ++i) o[i] = psum;
     float m = SHAPE == kCapped ? 0.0f : -INFINITY, l = 0.0f;
 
-    auto page_of = [&](int key) {   // -1: none
-        int p = -1;
-        if (key < keys.end) p = table[key >> a.cache.page_shift];
-        return (uint32_t)p < (uint32_t)a.cache.n_pages ? p : -1;
-    };
-    // the same of a group of 16 keys, for a whole wave (beyond the end: the last key's entry is read, and not used)
+    // Pages of a tile's groups of 16 keys (-1: none), looked up by scalar loads a tile before the states are fetched.  (Beyond the end the
+    // last key's entry is read, and not used.  Tiles begin at multiples of their length: a page that is as long holds all of one.)
+    typedef int Pages __attribute__((ext_vector_type(4)));   // (of a tile of 32 keys: two)
+    const bool one_page = (1 << a.cache.page_shift) >= TK;
     auto group_page = [&](int key) {
         const int p = table_entry(table, (key < keys.end ? key : keys.end - 1) >> a.cache.page_shift);
         return key < keys.end && (uint32_t)p < (uint32_t)a.cache.n_pages ? p : -1;
     };
-    // Pages of a tile, looked up a tile before its states are fetched: that of the wave's own rows (16 bits), and a bit for each group
-    // of 16 keys that has none.  (Tiles begin at multiples of their length: a page that is as long holds all of one.)
-    struct Pages {
-        int own, absent;
-    };
-    const bool one_page = (1 << a.cache.page_shift) >= TK;
     auto pages_of = [&](int key0) {
-        Pages p{-1, 0};
-        if (one_page && key0 + TK <= keys.end) {
-            p.own = group_page(key0);
-            p.absent = p.own < 0 ? (1 << (TK / 16)) - 1 : 0;
-        } else {
-            if (BITS == 16) p.own = group_page((key0 + wave * RW) & ~15);
-#pragma unroll
-            for (int g = 0; g < TK / 16; ++g) p.absent |= group_page(key0 + 16 * g) < 0 ? 1 << g : 0;
-        }
-        return p;
+        const int first = group_page(key0);
+        if (one_page && key0 + TK <= keys.end) return (Pages){first, first, first, first};
+        if constexpr (TK == 32) return (Pages){first, group_page(key0 + 16), -1, -1};
+        else return (Pages){first, group_page(key0 + 16), group_page(key0 + 32), group_page(key0 + 48)};
+    };
+    auto page_at = [](Pages p, int g) {
+        const int a = p[0], b = p[1], c = p[2], d = p[3];
+        const int low = g == 0 ? a : b, high = g == 2 ? c : d;
+        return TK == 32 || g < 2 ? low : high;
     };
     auto row_of = [&](int page, int key) {
         return (int64_t)page * a.cache.page_rows + ((int64_t)head << a.cache.page_shift) + (key & page_mask);
@@ -333,7 +324,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
         const int first = key0 + wave * RW;
         const uint32_t to = (uint32_t)(uintptr_t)(lds_void*)(side(buffer, 0) + wave * RW * (2 * D));
         const int64_t row0 = page < 0 ? 0 : row_of(page, first) * (2 * D);
-        if (page >= 0 && first + RW <= keys.end) {   // (one question a tile: asked at every load, the branches took longer than the loads)
+        if (page >= 0 && first >= keys.lo && first + RW <= keys.end) {   // (one question a tile: asked at every load, the branches took longer than the loads)
 #pragma unroll
             for (int i = 0; i < 2 * NI; ++i)
                 gemm::lds_dma16(to + (i / NI) * SIDE + (i % NI) * 1024, (i < NI ? a.cache.k : a.cache.v) + row0, offset[i / NI][i % NI]);
@@ -342,7 +333,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
             for (int which = 0; which < 2; ++which) {
 #pragma unroll
                 for (int i = 0; i < NI; ++i) {   // each lane's bytes land in the lane's place, whichever of the two copies takes them there
-                    if (page >= 0 && first + i * RI + lane / (D / 8) < keys.end)
+                    const int key = first + i * RI + lane / (D / 8);
+                    if (page >= 0 && key >= keys.lo && key < keys.end)
                         gemm::lds_dma16(to + which * SIDE + i * 1024, (which ? a.cache.v : a.cache.k) + row0, which ? offset[1][i] : offset[0][i]);
                     else
                         gemm::lds_dma16(to + which * SIDE + i * 1024, no_state, 16 * (lane % (D / 8)));
@@ -356,8 +348,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
     const Widen<BITS> widen;
     uint32_t raw[2][CW];
     float raw_scale = 0.0f;
-    auto fetch_codes = [&](int key0) {
-        const int key = key0 + chunk_row, page = page_of(key);
+    auto fetch_codes = [&](int key0, Pages p) {
+        const int key = key0 + chunk_row, page = key >= keys.lo && key < keys.end ? page_at(p, chunk_row / 16) : -1;
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
             if (!BOTH && which == 1) continue;
@@ -368,8 +360,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
         }
         raw_scale = 0.0f;
         if ((int)threadIdx.x < 2 * TK) {
-            const int k = key0 + (int)(threadIdx.x % TK), p = page_of(k);
-            if (p >= 0) raw_scale = (int)threadIdx.x < TK ? a.cache.k_scales[row_of(p, k)] * factor : a.cache.v_scales[row_of(p, k)];
+            const int in_tile = threadIdx.x % TK, k = key0 + in_tile, scale_page = page_at(p, in_tile / 16);
+            if (scale_page >= 0 && k >= keys.lo && k < keys.end)
+                raw_scale = (int)threadIdx.x < TK ? a.cache.k_scales[row_of(scale_page, k)] : a.cache.v_scales[row_of(scale_page, k)];
         }
     };
     auto store_codes = [&](int buffer) {
@@ -383,19 +376,19 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
                 *reinterpret_cast<u32x4*>(side(buffer, values) + place) = widen(raw[which], g);
             }
         }
-        if ((int)threadIdx.x < 2 * TK) scales[buffer * 2 * TK + threadIdx.x] = raw_scale;
+        if ((int)threadIdx.x < 2 * TK) scales[buffer * 2 * TK + threadIdx.x] = (int)threadIdx.x < TK ? raw_scale * factor : raw_scale;
     };
 
-    Pages pages{-1, 0}, next_pages{-1, 0};
+    Pages pages = {-1, -1, -1, -1}, next_pages = pages;
     if (mine.from < mine.to) {
         const int key0 = keys.base + mine.from * TK;
         pages = pages_of(key0);
         next_pages = pages_of(key0 + TK);
         if constexpr (CODES) {
-            fetch_codes(key0);
+            fetch_codes(key0, pages);
             store_codes(0);
         } else {
-            fetch16(key0, pages.own, 0);
+            fetch16(key0, page_at(pages, wave * RW / 16), 0);
         }
     }
     gemm::wait_loads_then_barrier<0>();
@@ -403,10 +396,11 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
         const int buffer = (t - mine.from) & 1, key0 = keys.base + t * TK;
         const bool more = t + 1 < mine.to;
         if (more) {
-            if constexpr (CODES) fetch_codes(key0 + TK);
-            else fetch16(key0 + TK, next_pages.own, buffer ^ 1);
+            if constexpr (CODES) fetch_codes(key0 + TK, next_pages);
+            else fetch16(key0 + TK, page_at(next_pages, wave * RW / 16), buffer ^ 1);
         }
-        const int absent = pages.absent;
+        // groups of 16 keys without a page
+        const int absent = (pages[0] < 0 ? 1 : 0) | (pages[1] < 0 ? 2 : 0) | (TK == 64 && pages[2] < 0 ? 4 : 0) | (TK == 64 && pages[3] < 0 ? 8 : 0);
         pages = next_pages;
         next_pages = pages_of(key0 + 2 * TK);
         if (key0 < any_hi && key0 + TK > any_lo) {
@@ -495,13 +489,13 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_prefill_kern
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float x = score[b][4 * j + i];
-                        e[i] = __builtin_amdgcn_exp2f(CODES || SHAPE != kScaled ? x + ref : __builtin_fmaf(x, step, ref));
+                        e[i] = __builtin_amdgcn_exp2f(SHAPE == kCapped ? x : CODES || SHAPE != kScaled ? x + ref : __builtin_fmaf(x, step, ref));
                         l += e[i];
                     }
                     if constexpr (CODES) {
                         const f32x4 vs = *reinterpret_cast<const f32x4*>(scales + buffer * 2 * TK + TK + 32 * b + 8 * j + 4 * half);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) e[i] = plain || e[i] > 0.0f ? e[i] * vs[i] : 0.0f;
+                        for (int i = 0; i < 4; ++i) e[i] *= vs[i];   // (of what no row sees the scale here is 0)
                     }
                     w[2 * j] = pack_bf16(e[0], e[1]);
                     w[2 * j + 1] = pack_bf16(e[2], e[3]);
@@ -609,8 +603,8 @@ int64_t most_row_tiles(int64_t T, int n_seqs, int group) {
 }
 // Workgroups that the chip's 256 CUs hold at once, and units that a call with parts may have (a bit less than two rounds: the
 // workspace then is 66 MB at most).
-constexpr int round_of(int d) { return d == 256 ? 256 : 512; }
-constexpr int most_units(int d) { return d == 256 ? 500 : 1000; }
+constexpr int round_of(int d) { return d == 256 ? 256 : d == 64 ? 768 : 512; }
+constexpr int most_units(int d) { return d == 256 ? 500 : d == 64 ? 1500 : 1000; }
 // Whether keys are cut: if there may be units for it.
 bool cut_keys(int64_t T, int n_seqs, int group, int heads, int d) {
     return n_seqs <= kMostSplitSeqs && most_row_tiles(T, n_seqs, group) * heads < most_units(d);

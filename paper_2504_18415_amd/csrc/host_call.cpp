@@ -26,17 +26,22 @@ struct Library {
     decltype(&hbl_kv_quant_absmax) kv_quant;
     decltype(&hbl_kv_dequant) kv_dequant;
     decltype(&hbl_kv_packed_bytes) kv_packed_bytes;
+    decltype(&hbl_rope) rope;
+    decltype(&hbl_kv_append) kv_append;
+    decltype(&hbl_paged_attention) attention;
+    decltype(&hbl_paged_attention_workspace_bytes) attention_workspace;
 } lib;
 
 PyObject* decline() { Py_RETURN_NONE; }
 
-// A plain contiguous device tensor with memory of its own: nothing that a mode, a transform or a subclass stands behind.
-bool ordinary(const at::Tensor& t) {
+// A plain device tensor with memory of its own: nothing that a mode, a transform or a subclass stands behind.
+bool plain(const at::Tensor& t) {
     using K = c10::DispatchKey;
     static const c10::DispatchKeySet other({K::Python, K::PythonTLSSnapshot, K::Functionalize, K::FuncTorchBatched,
                                             K::FuncTorchGradWrapper, K::Batched, K::Conjugate, K::Negative, K::ZeroTensor});
-    return t.defined() && t.is_cuda() && t.layout() == c10::kStrided && t.has_storage() && !t.key_set().has_any(other) && t.is_contiguous();
+    return t.defined() && t.is_cuda() && t.layout() == c10::kStrided && t.has_storage() && !t.key_set().has_any(other);
 }
+bool ordinary(const at::Tensor& t) { return plain(t) && t.is_contiguous(); }
 // The tensor behind a Python object, or nullptr if it is not an ordinary one.  (torch.Tensor and Parameter, no other subclass.)
 const at::Tensor* tensor(PyObject* o) {
     if (!THPVariable_CheckExact(o)) return nullptr;
@@ -250,14 +255,151 @@ PyObject* kv_dequant(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// Head states [T, H, d] on the current device: heads contiguous, tokens `stride` values apart.
+struct Heads {
+    const at::Tensor* t = nullptr;
+    int64_t T = 0, H = 0, d = 0, stride = 0;
+    int dtype = HBL_BF16;
+};
+bool get_heads(PyObject* o, Heads& h) {
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!plain(t) || t.dim() != 3 || t.get_device() != c10::hip::current_device()) return false;
+    h.t = &t;
+    h.T = t.size(0);
+    h.H = t.size(1);
+    h.d = t.size(2);
+    h.dtype = x_dtype(t);
+    h.stride = h.T > 1 ? t.stride(0) : h.H * h.d;
+    return h.dtype >= 0 && h.T > 0 && h.H > 0 && h.d > 1 && t.stride(2) == 1 && (h.H == 1 || t.stride(1) == h.d) && h.stride >= h.H * h.d;
+}
+bool same_shape(const Heads& a, const Heads& b) { return a.T == b.T && a.H == b.H && a.d == b.d; }
+// A contiguous tensor of that type and length, where `on` is.
+const at::Tensor* vector(PyObject* o, at::ScalarType type, int64_t numel, const at::Tensor& on) {
+    const at::Tensor* t = tensor(o);
+    return t && t->scalar_type() == type && t->numel() == numel && t->get_device() == on.get_device() ? t : nullptr;
+}
+// A KvCache as (its struct's address, its device's index).
+struct Cache {
+    const hbl_kv_cache* c = nullptr;
+};
+bool get_cache(PyObject* o, int64_t device, Cache& cache) {
+    if (!PyTuple_CheckExact(o) || PyTuple_GET_SIZE(o) != 2) return false;
+    int64_t index;
+    if (!get_int(PyTuple_GET_ITEM(o, 1), index) || index != device) return false;
+    cache.c = static_cast<const hbl_kv_cache*>(PyLong_AsVoidPtr(PyTuple_GET_ITEM(o, 0)));
+    return cache.c != nullptr;
+}
+bool get_batch(PyObject* starts, PyObject* lens, PyObject* table, const at::Tensor& on, hbl_kv_batch& b) {
+    const at::Tensor* l = tensor(lens);
+    if (!l || l->scalar_type() != at::kInt || l->get_device() != on.get_device() || !THPVariable_CheckExact(table)) return false;
+    const int64_t n = l->numel();
+    const at::Tensor* s = vector(starts, at::kInt, n + 1, on);
+    const at::Tensor& t = THPVariable_Unpack(table);
+    if (!s || !plain(t) || t.scalar_type() != at::kInt || t.dim() != 2 || t.get_device() != on.get_device() || n < 1 || n > (1 << 20) ||
+        t.size(0) != n || t.size(1) < 1 || t.size(1) > (1 << 26) || t.stride(1) != 1 || (n > 1 && t.stride(0) < t.size(1)))
+        return false;
+    b = hbl_kv_batch{s->const_data_ptr<int32_t>(), l->const_data_ptr<int32_t>(), t.const_data_ptr<int32_t>(), n > 1 ? t.stride(0) : t.size(1), (int)n,
+                     (int)t.size(1)};
+    return true;
+}
+
+// rope(x, positions, freqs, layout, magnitude, backward, out type (0 fp32, 1 bf16, -1 that of x), out)
+PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Heads x, given;
+    int64_t layout, type;
+    float magnitude;
+    if (n != 8 || !get_heads(a[0], x) || !get_int(a[3], layout) || !get_float(a[4], magnitude) || !PyBool_Check(a[5]) || !get_int(a[6], type))
+        return decline();
+    const at::Tensor *positions = vector(a[1], at::kInt, x.T, *x.t), *freqs = tensor(a[2]);
+    if (!positions || !freqs || !vector(a[2], at::kFloat, freqs->numel(), *x.t)) return decline();
+    if (a[7] != Py_None && (!get_heads(a[7], given) || !same_shape(given, x))) return decline();
+    const int out_dtype = given.t ? given.dtype : type < 0 ? x.dtype : (int)type;
+    const int backward = a[5] == Py_True;
+    at::Tensor out;
+    void* s = stream();
+    const int rc = without_gil([&] {
+        out = given.t ? *given.t : at::empty({x.T, x.H, x.d}, x.t->options().dtype(out_dtype == HBL_BF16 ? at::kBFloat16 : at::kFloat));
+        if (!plain(out)) return kDeclined;
+        return lib.rope(input(*x.t), x.dtype, x.T, x.H, x.d, x.stride, positions->const_data_ptr<int32_t>(), floats(*freqs), 2 * freqs->numel(),
+                        (int)layout, magnitude, backward, out.data_ptr(), out_dtype, given.t ? given.stride : x.H * x.d, s);
+    });
+    return result(rc, a[7], out);
+    END_HANDLE_TH_ERRORS
+}
+
+// kv_append(cache, k, v, q_starts, kv_lens, block_table, freqs or None, layout, magnitude, q, q_out or None, eps): calls with queries
+PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Heads k, v, q, given;
+    Cache cache;
+    hbl_kv_batch batch;
+    int64_t layout;
+    float magnitude, eps;
+    if (n != 12 || !get_heads(a[1], k) || !get_heads(a[2], v) || !same_shape(k, v) || k.dtype != v.dtype || !get_heads(a[9], q) || q.T != k.T ||
+        q.d != k.d || q.dtype != k.dtype || !get_cache(a[0], k.t->get_device(), cache) || cache.c->n_kv_heads != k.H || cache.c->d != k.d ||
+        !get_batch(a[3], a[4], a[5], *k.t, batch) || !get_int(a[7], layout) || !get_float(a[8], magnitude) || !get_float(a[11], eps))
+        return decline();
+    const at::Tensor* freqs = nullptr;
+    if (a[6] != Py_None && (!(freqs = tensor(a[6])) || !vector(a[6], at::kFloat, freqs->numel(), *k.t))) return decline();
+    if (a[10] != Py_None && (!get_heads(a[10], given) || !same_shape(given, q))) return decline();
+    const int out_dtype = given.t ? given.dtype : q.dtype;
+    at::Tensor out;
+    void* s = stream();
+    const int rc = without_gil([&] {
+        out = given.t ? *given.t : at::empty({q.T, q.H, q.d}, q.t->options());
+        if (!plain(out)) return kDeclined;
+        return lib.kv_append(cache.c, &batch, input(*k.t), k.stride, input(*v.t), v.stride, k.dtype, k.T, input(*q.t), q.H, q.stride, out.data_ptr(),
+                             out_dtype, given.t ? given.stride : q.H * q.d, freqs ? floats(*freqs) : nullptr, freqs ? 2 * freqs->numel() : 0,
+                             (int)layout, magnitude, eps, s);
+    });
+    return result(rc, a[10], out);
+    END_HANDLE_TH_ERRORS
+}
+
+// attention(cache, q, q_starts, kv_lens, block_table, max_q_len, scale, softcap, window, slopes, prefix_lens, out, workspace): the last
+// four may be None
+PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Heads q, given;
+    Cache cache;
+    hbl_kv_batch batch;
+    int64_t max_q, window;
+    float scale, softcap;
+    if (n != 13 || !get_heads(a[1], q) || q.dtype != HBL_BF16 || !get_cache(a[0], q.t->get_device(), cache) || cache.c->d != q.d ||
+        !get_batch(a[2], a[3], a[4], *q.t, batch) || !get_int(a[5], max_q) || !get_float(a[6], scale) || !get_float(a[7], softcap) ||
+        !get_int(a[8], window))
+        return decline();
+    const at::Tensor *slopes = nullptr, *prefix = nullptr, *kept = nullptr;
+    if (a[9] != Py_None && !(slopes = vector(a[9], at::kFloat, q.H, *q.t))) return decline();
+    if (a[10] != Py_None && !(prefix = vector(a[10], at::kInt, batch.n_seqs, *q.t))) return decline();
+    if (a[11] != Py_None && (!get_heads(a[11], given) || !same_shape(given, q) || given.dtype != HBL_BF16)) return decline();
+    if (a[12] != Py_None && (!(kept = tensor(a[12])) || kept->scalar_type() != at::kByte || kept->get_device() != q.t->get_device())) return decline();
+    at::Tensor out, workspace;
+    void* s = stream();
+    const int rc = without_gil([&] {
+        out = given.t ? *given.t : at::empty({q.T, q.H, q.d}, q.t->options());
+        if (kept) workspace = *kept;
+        else workspace = at::empty({(int64_t)lib.attention_workspace(cache.c, &batch, q.T, q.H, max_q)}, q.t->options().dtype(at::kByte));
+        if (!plain(out) || !ordinary(workspace)) return kDeclined;
+        return lib.attention(input(*q.t), q.T, q.H, q.stride, cache.c, &batch, max_q, scale, softcap, window, slopes ? floats(*slopes) : nullptr,
+                             prefix ? prefix->const_data_ptr<int32_t>() : nullptr, out.data_ptr(), given.t ? given.stride : q.H * q.d,
+                             workspace.data_ptr(), workspace.numel(), s);
+    });
+    return result(rc, a[11], out);
+    END_HANDLE_TH_ERRORS
+}
+
 // bind(addresses of the library's functions, in the order of `Library`)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    void* f[9];
-    if (n != 9) {
-        PyErr_SetString(PyExc_TypeError, "nine addresses");
+    constexpr int kFunctions = 13;
+    void* f[kFunctions];
+    if (n != kFunctions) {
+        PyErr_SetString(PyExc_TypeError, "thirteen addresses");
         return nullptr;
     }
-    for (int i = 0; i < 9; ++i) {
+    for (int i = 0; i < kFunctions; ++i) {
         f[i] = PyLong_AsVoidPtr(a[i]);
         if (f[i] == nullptr) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null address");
@@ -268,13 +410,16 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
                   reinterpret_cast<decltype(&hbl_ln_bitlinear_forward)>(f[2]), reinterpret_cast<decltype(&hbl_bitlinear_forward_small)>(f[3]),
                   reinterpret_cast<decltype(&hbl_workspace_bytes)>(f[4]), reinterpret_cast<decltype(&hbl_fwht)>(f[5]),
                   reinterpret_cast<decltype(&hbl_kv_quant_absmax)>(f[6]), reinterpret_cast<decltype(&hbl_kv_dequant)>(f[7]),
-                  reinterpret_cast<decltype(&hbl_kv_packed_bytes)>(f[8])};
+                  reinterpret_cast<decltype(&hbl_kv_packed_bytes)>(f[8]), reinterpret_cast<decltype(&hbl_rope)>(f[9]),
+                  reinterpret_cast<decltype(&hbl_kv_append)>(f[10]), reinterpret_cast<decltype(&hbl_paged_attention)>(f[11]),
+                  reinterpret_cast<decltype(&hbl_paged_attention_workspace_bytes)>(f[12])};
     Py_RETURN_NONE;
 }
 
 #define HBL_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {HBL_METHOD(bind), HBL_METHOD(forward), HBL_METHOD(ln_forward), HBL_METHOD(small), HBL_METHOD(fwht),
-                         HBL_METHOD(kv_quant), HBL_METHOD(kv_dequant), {nullptr, nullptr, 0, nullptr}};
+                         HBL_METHOD(kv_quant), HBL_METHOD(kv_dequant), HBL_METHOD(rope), HBL_METHOD(kv_append),
+                         HBL_METHOD(attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -154,7 +154,8 @@ def _bind_native(L):
         return
     _host_call.bind(*[ctypes.cast(f, ctypes.c_void_p).value for f in (
         L.hbl_hbitlinear_forward, L.hbl_plain_bitlinear_forward, L.hbl_ln_bitlinear_forward, L.hbl_bitlinear_forward_small,
-        L.hbl_workspace_bytes, L.hbl_fwht, L.hbl_kv_quant_absmax, L.hbl_kv_dequant, L.hbl_kv_packed_bytes)])
+        L.hbl_workspace_bytes, L.hbl_fwht, L.hbl_kv_quant_absmax, L.hbl_kv_dequant, L.hbl_kv_packed_bytes, L.hbl_rope, L.hbl_kv_append,
+        L.hbl_paged_attention, L.hbl_paged_attention_workspace_bytes)])
     _call = _host_call
 
 
@@ -638,6 +639,8 @@ def _heads_out(out, like, dtype, what: str):
     """``out`` for head states shaped as ``like``: given, or allocated.  -> (out, token stride)"""
     if out is None:
         T, H, d = like.shape
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise TypeError(f"{what} must be torch.bfloat16 or torch.float32")
         return torch.empty((T, H, d), dtype=dtype, device=like.device), H * d
     if out.shape != like.shape or out.device != like.device:
         raise ValueError(f"{what} must be {tuple(like.shape)} on {like.device} (got {tuple(out.shape)} on {out.device})")
@@ -659,13 +662,17 @@ def rope(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, layout: 
     """Rotary positions of head states x [T, H, d] (a slice of a fused QKV output is taken where it is): the first
     2 * len(freqs) features of every head turn by positions[t] * freqs[i].  ``backward``: the transposed map, from dL/dy to
     dL/dx.  ``out`` may be ``x`` itself."""
+    layout = _choice(ROPE_LAYOUTS, "layout", layout)
+    if _call is not None and (out_dtype is None or out_dtype in (torch.float32, torch.bfloat16)):
+        r = _call.rope(x, positions, freqs, layout, magnitude, backward, -1 if out_dtype is None else int(out_dtype is torch.bfloat16), out)
+        if r is not None:
+            return r if type(r) is not int else _check(r, "rope")
     T, H, d, stride = _heads(x, "x")
     _index(positions, "positions", T, x.device)
     _floats(freqs, "freqs", freqs.numel(), x.device)
     out, out_stride = _heads_out(out, x, out_dtype or x.dtype, "out")
     _check(lib().hbl_rope(_ptr(x), _x_dtype(x), T, H, d, stride, _ptr(positions), _ptr(freqs), 2 * freqs.numel(),
-                          _choice(ROPE_LAYOUTS, "layout", layout), magnitude, int(bool(backward)), _ptr(out), _x_dtype(out),
-                          out_stride, _stream()), "rope")
+                          layout, magnitude, int(bool(backward)), _ptr(out), _x_dtype(out), out_stride, _stream()), "rope")
     return out
 
 
@@ -703,6 +710,7 @@ class KvCache:
         self.n_pages, self.n_kv_heads, self.page_size, self.d = n_pages, heads, page, d
         self._c = _Cache(_ptr(k), _ptr(v), _ptr(k_scales), _ptr(v_scales), n_pages, page_rows, bits, page, heads, d)
         self._ref = ctypes.byref(self._c)
+        self._native = (ctypes.addressof(self._c), k.device.index)
 
     @classmethod
     def empty(cls, n_pages: int, n_kv_heads: int, page_size: int, d: int, bits: int = 16, device="cuda") -> "KvCache":
@@ -737,6 +745,11 @@ def kv_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, q_starts: torch.
 
     The batch: sequence s has the tokens [q_starts[s], q_starts[s+1]), the last ones of its kv_lens[s] keys (these included);
     its key j lies in page block_table[s][j // page size].  All int32 on the device, read by the kernel."""
+    layout = _choice(ROPE_LAYOUTS, "layout", layout)
+    if _call is not None and q is not None:
+        r = _call.kv_append(cache._native, k, v, q_starts, kv_lens, block_table, freqs, layout, magnitude, q, q_out, eps)
+        if r is not None:
+            return r if type(r) is not int else _check(r, "kv_append")
     T, H, d, k_stride = _heads(k, "k")
     if H != cache.n_kv_heads or d != cache.d or k.device != cache.k.device:
         raise ValueError(f"k must be [T, {cache.n_kv_heads}, {cache.d}] on {cache.k.device} (got {tuple(k.shape)} on {k.device})")
@@ -758,7 +771,7 @@ def kv_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, q_starts: torch.
     batch = _batch(cache, q_starts, kv_lens, block_table)
     _check(lib().hbl_kv_append(cache._ref, ctypes.byref(batch), _ptr(k), k_stride, _ptr(v), v_stride, _x_dtype(k), T, _ptr(q), Hq, q_stride,
                                _ptr(q_out), BF16 if q is None else _x_dtype(q_out), q_out_stride, _ptr(freqs), rot,
-                               _choice(ROPE_LAYOUTS, "layout", layout), magnitude, eps, _stream()), "kv_append")
+                               layout, magnitude, eps, _stream()), "kv_append")
     return q_out
 
 
@@ -775,6 +788,13 @@ def paged_attention(q: torch.Tensor, cache: KvCache, q_starts: torch.Tensor, kv_
     The batch as for :func:`kv_append`; ``max_q_len`` is at least the new tokens of any sequence; ``scale`` is 1/sqrt(d) where
     not given.  ``softcap``: scores capped by a tanh; ``window``: keys so far back only; ``slopes`` [query heads] fp32: a bias by
     distance; ``prefix_lens`` [sequences] int32: the keys that every token sees.  A token that sees nothing gets zeros."""
+    if scale is None:
+        scale = cache.d ** -0.5
+    if _call is not None:
+        r = _call.attention(cache._native, q, q_starts, kv_lens, block_table, max_q_len, scale, softcap, window, slopes, prefix_lens, out,
+                            workspace)
+        if r is not None:
+            return r if type(r) is not int else _check(r, "paged_attention")
     T, Hq, d, q_stride = _heads(q, "q")
     if q.dtype != torch.bfloat16:
         raise TypeError("q must be torch.bfloat16")
@@ -795,6 +815,6 @@ def paged_attention(q: torch.Tensor, cache: KvCache, q_starts: torch.Tensor, kv_
     elif workspace.dtype != torch.uint8 or workspace.device != q.device or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous uint8 device tensor")
     _check(L.hbl_paged_attention(_ptr(q), T, Hq, q_stride, cache._ref, ctypes.byref(batch), max_q_len,
-                                 d ** -0.5 if scale is None else scale, softcap, window, _ptr(slopes), _ptr(prefix_lens), _ptr(out),
+                                 scale, softcap, window, _ptr(slopes), _ptr(prefix_lens), _ptr(out),
                                  out_stride, _ptr(workspace), workspace.numel(), _stream()), "paged_attention")
     return out

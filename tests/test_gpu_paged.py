@@ -446,3 +446,92 @@ def test_two_streams_at_once(hbl):
     for i in range(2):
         for y in got[i]:
             assert torch.equal(y.view(torch.int16), want[i].view(torch.int16))
+
+
+# --- the binding ------------------------------------------------------------------------------------------------
+
+def test_native_and_python_marshalling_agree(hbl, monkeypatch):
+    """Both ways of making the calls: the same outputs bit for bit, and the same refusals."""
+    note("native and Python marshalling")
+    native = hbl._call
+    assert native is not None, "_host_call is not built"
+    g = gen(71)
+    T, Hq, Hkv, d, page, bits = 20, 4, 2, 64, 16, 8
+    qkv = torch.randn((T, (Hq + 2 * Hkv) * d), generator=g).bfloat16().cuda()
+    q, k, v = (p.unflatten(-1, (-1, d)) for p in qkv.split((Hq * d, Hkv * d, Hkv * d), -1))
+    table, starts, lens = torch.randperm(8, generator=g).to(torch.int32).cuda().view(2, 4), ints([0, 13, 20]), ints([40, 7])
+    freqs, positions = hbl.rope_frequencies(d), torch.arange(T, dtype=torch.int32, device="cuda")
+    slopes, prefix = torch.tensor([0.5, 0.25, 0.125, 0.0], device="cuda"), ints([20, 0])
+
+    def outputs():
+        cache = hbl.KvCache.empty(8, Hkv, page, d, bits)
+        for t in (cache.k, cache.v, cache.k_scales, cache.v_scales):
+            t.zero_()
+        yield hbl.rope(q, positions, freqs)
+        yield hbl.rope(q, positions, freqs, "interleaved", 1.5, True, torch.float32)
+        kept = torch.zeros((T, 2 * Hq, d), dtype=torch.float32, device="cuda")
+        assert hbl.rope(q, positions, freqs, out=kept[:, Hq:]).data_ptr() == kept[:, Hq:].data_ptr()
+        yield kept
+        turned = hbl.kv_append(cache, k, v, starts, lens, table, freqs=freqs, q=q)
+        yield turned
+        assert hbl.kv_append(cache, k, v, starts, lens, table) is None
+        yield hbl.kv_append(cache, k, v, starts, lens, table, freqs=freqs, layout="interleaved", q=q, q_out=torch.zeros_like(kept[:, :Hq]))
+        yield from (cache.k, cache.v, cache.k_scales, cache.v_scales)
+        yield hbl.paged_attention(turned, cache, starts, lens, table, 13)
+        n = hbl.paged_attention_workspace_bytes(cache, T, 2, Hq, 13)
+        yield hbl.paged_attention(turned, cache, starts, lens, table, 13, scale=0.2, softcap=5.0, window=9, slopes=slopes, prefix_lens=prefix,
+                                  out=torch.zeros_like(turned), workspace=torch.empty(n, dtype=torch.uint8, device="cuda"))
+
+    mine = list(outputs())
+    monkeypatch.setattr(hbl, "_call", None)
+    for a, b in zip(mine, outputs(), strict=True):
+        assert a.dtype == b.dtype and torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    cache = hbl.KvCache.empty(8, Hkv, page, d, bits)
+    for call in (native, None):
+        monkeypatch.setattr(hbl, "_call", call)
+        refused = [
+            (ValueError, lambda: hbl.rope(q.transpose(0, 1), positions, freqs)), (ValueError, lambda: hbl.rope(q, positions[:5], freqs)),
+            (ValueError, lambda: hbl.rope(q, positions.long(), freqs)), (ValueError, lambda: hbl.rope(q, positions, freqs.double())),
+            (ValueError, lambda: hbl.rope(q, positions, freqs.cpu())), (ValueError, lambda: hbl.rope(q, positions, freqs, layout="both")),
+            (TypeError, lambda: hbl.rope(q.half(), positions, freqs)), (TypeError, lambda: hbl.rope(q, positions, freqs, out_dtype=torch.float16)),
+            (ValueError, lambda: hbl.rope(q, positions, freqs, out=torch.empty_like(q)[:, :2])),
+            (hbl.HblError, lambda: hbl.rope(q, positions, freqs[:4].clone())), (hbl.HblError, lambda: hbl.rope(q, positions, hbl.rope_frequencies(128))),
+            (ValueError, lambda: hbl.kv_append(cache, k[:, :1], v[:, :1], starts, lens, table)), (ValueError, lambda: hbl.kv_append(cache, k, v[:5], starts, lens, table)),
+            (ValueError, lambda: hbl.kv_append(cache, k, v, starts[:2], lens, table, q=q)), (ValueError, lambda: hbl.kv_append(cache, k, v, starts, lens, table.t(), q=q)),
+            (ValueError, lambda: hbl.kv_append(cache, k, v, starts, lens, table, q=q.float())), (ValueError, lambda: hbl.kv_append(cache, k, v, starts, lens, table, q_out=q)),
+            (ValueError, lambda: hbl.kv_append(cache, k, v, starts, lens, table[:1], q=q)),
+            (TypeError, lambda: hbl.paged_attention(q.float(), cache, starts, lens, table, 13)), (ValueError, lambda: hbl.paged_attention(q, cache, starts, lens.long(), table, 13)),
+            (ValueError, lambda: hbl.paged_attention(q, cache, starts, lens, table, 13, slopes=slopes[:3])),
+            (ValueError, lambda: hbl.paged_attention(q, cache, starts, lens, table, 13, prefix_lens=prefix[:1])),
+            (hbl.HblError, lambda: hbl.paged_attention(q[:, :3].contiguous(), cache, starts, lens, table, 13)),
+            (hbl.HblError, lambda: hbl.paged_attention(q, cache, starts, lens, table, 0)), (hbl.HblError, lambda: hbl.paged_attention(q, cache, starts, lens, table, 13, window=-1)),
+            (hbl.HblError, lambda: hbl.paged_attention(q, cache, starts, lens, table, 13, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))),
+            (ValueError, lambda: hbl.KvCache(cache.k, cache.v, 16)), (ValueError, lambda: hbl.KvCache(cache.k, cache.v, 8)),
+            (ValueError, lambda: hbl.KvCache(cache.k, cache.v[:4], 8, cache.k_scales, cache.v_scales)),
+            (ValueError, lambda: hbl.KvCache(cache.k, cache.v, 5, cache.k_scales, cache.v_scales)),
+            (ValueError, lambda: hbl.KvCache(cache.k.transpose(1, 2), cache.v, 8, cache.k_scales, cache.v_scales))]
+        for i, (error, f) in enumerate(refused):
+            with pytest.raises(error):
+                f()
+                print("not refused:", i)
+
+
+def test_empty_calls(hbl):
+    note("empty calls")
+    cache, table = hbl.KvCache.empty(2, 2, 16, 64), torch.zeros((0, 3), dtype=torch.int32, device="cuda")
+    x = torch.zeros((0, 2, 64), dtype=torch.bfloat16, device="cuda")
+    assert hbl.rope(x, ints([]), hbl.rope_frequencies(64)).shape == (0, 2, 64)
+    assert hbl.kv_append(cache, x, x, ints([0]), ints([]), table, q=x).shape == (0, 2, 64)
+    assert hbl.paged_attention(x, cache, ints([0]), ints([]), table, 1).shape == (0, 2, 64)
+    # tokens of nobody, a cache without pages, a table without columns
+    y = torch.ones((3, 2, 64), dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(y, 7.0)
+    hbl.paged_attention(y, cache, ints([0]), ints([]), table, 1, out=out)
+    assert (out == 7.0).all()
+    none, narrow = hbl.KvCache.empty(0, 2, 16, 64), torch.zeros((1, 0), dtype=torch.int32, device="cuda")
+    for c, t in ((none, torch.zeros((1, 3), dtype=torch.int32, device="cuda")), (cache, narrow)):
+        if c.n_pages:
+            hbl.kv_append(c, y, y, ints([0, 3]), ints([3]), t)
+            for n in (3, 40):
+                out = hbl.paged_attention(y, c, ints([0, 3]), ints([3]), t, n)
+                assert (out == 0).all()

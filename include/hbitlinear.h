@@ -379,7 +379,7 @@ typedef struct hbl_kv_cache {
  * j mod page_size of page block_table[s * table_stride + j / page_size].
  *   q_starts [n_seqs + 1] and kv_lens [n_seqs] int32, q_starts not decreasing;  block_table [n_seqs] rows of table_width
  * An entry of the table outside [0, n_pages) stands for no page: nothing is written there, and its keys are left out of the
- * attention (a window may have passed them).  Keys beyond table_width pages do not exist.  Tokens outside every sequence,
+ * attention (a window may have passed them).  Keys beyond table_width pages (or 2^31 - 4096) do not exist.  Tokens outside every sequence,
  * [0, q_starts[0]) and [q_starts[n_seqs], T), are left as they were.
  */
 typedef struct hbl_kv_batch {
@@ -415,7 +415,7 @@ int hbl_kv_append(const hbl_kv_cache* cache, const hbl_kv_batch* batch, const vo
  * weights are rounded to bf16 for the product with the values.
  *   q, out          [T, n_q_heads, d] bf16 with strides in values as for hbl_rope; they must not overlap
  *   max_q_len       at least the new tokens of any sequence (those beyond it are left as they were)
- *   sizes           T n_q_heads < 2^31, n_seqs n_kv_heads table_width page_size < 2^38
+ *   sizes           T n_q_heads < 2^31, n_seqs n_kv_heads (table_width page_size + 256) < 2^38
  *   window >= 0;  slopes device [n_q_heads] fp32 or NULL;  prefix_lens device [n_seqs] int32 or NULL
  *   workspace       device, >= hbl_paged_attention_workspace_bytes(same arguments), 256-byte aligned; nothing in it has to
  *                   start at a value; calls that may overlap need one each

@@ -536,6 +536,7 @@ int hbl_test_gemm_i32_tile(const void* codes, int code_form, int64_t T, int64_t 
 namespace {
 
 constexpr int64_t kMostTokens = 1 << 24, kMostValues = (int64_t)1 << 40;   // (values between two tokens times tokens)
+constexpr int64_t kMostKeys = 0x7FFFF000;   // of a sequence: a few tiles more still are 32-bit numbers
 
 bool dtype_ok(int t) { return t == HBL_F32 || t == HBL_BF16; }
 int value_bytes(int t) { return t == HBL_BF16 ? 2 : 4; }
@@ -584,7 +585,7 @@ PagedCache paged_cache(const hbl_kv_cache* c) {
 PagedBatch paged_batch(const hbl_kv_batch* b, const hbl_kv_cache* c) {
     // (a cache without pages has no keys: nothing looks for one)
     const int64_t keys = c->n_pages > 0 ? (int64_t)b->table_width * c->page_size : 0;
-    return {b->q_starts, b->kv_lens, b->block_table, b->table_stride, b->n_seqs, (int)(keys < 0x7FFFFFFF ? keys : 0x7FFFFFFF)};
+    return {b->q_starts, b->kv_lens, b->block_table, b->table_stride, b->n_seqs, (int)(keys < kMostKeys ? keys : kMostKeys)};
 }
 // Sizes of an attention call (nothing here is read through a pointer).
 int check_attention_shape(const hbl_kv_cache* c, const hbl_kv_batch* b, int64_t T, int64_t Hq, int64_t max_q_len) {
@@ -592,8 +593,8 @@ int check_attention_shape(const hbl_kv_cache* c, const hbl_kv_batch* b, int64_t 
     if (rc == HBL_OK) rc = check_batch(b, T);
     if (rc != HBL_OK) return rc;
     if (Hq < 1 || Hq > (1 << 16) || Hq % c->n_kv_heads != 0 || max_q_len < 1 || T * Hq > 0x7FFFFFFF) return HBL_E_SHAPE;
-    // (tiles of keys are counted in 32 bits)
-    if ((double)b->n_seqs * c->n_kv_heads * b->table_width * c->page_size >= (double)((int64_t)1 << 38)) return HBL_E_SHAPE;
+    // (tiles of keys, and pairs of sequence and head, are counted in 32 bits)
+    if ((double)b->n_seqs * c->n_kv_heads * ((double)b->table_width * c->page_size + 256.0) >= (double)((int64_t)1 << 38)) return HBL_E_SHAPE;
     return HBL_OK;
 }
 

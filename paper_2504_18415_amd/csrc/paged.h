@@ -25,7 +25,7 @@ struct PagedBatch {
     const int32_t* block_table;   // [n_seqs][table_stride]
     int64_t table_stride;
     int n_seqs;
-    int capacity;                 // keys that a row of the table has pages for (up to 2^31 - 1)
+    int capacity;                 // keys that a row of the table has pages for (at most 2^31 - 4096)
 };
 
 // Sequence s as the kernels take it: tokens [first, first + n) inside the call's T, `keys` inside its row of the table.  `total` is

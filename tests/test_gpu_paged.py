@@ -126,6 +126,10 @@ def test_append(hbl, case, d, rot, bits, dtype, layout):
     q_out = torch.full((T, Hq, d), 7.0, dtype=dtype, device="cuda")
     got = hbl.kv_append(cache, k, v, ints(starts), ints(lens), table.cuda(), freqs=freqs, layout=layout, q=q, q_out=q_out)
     assert got is q_out
+    # once more, the queries where they are: the same rows again
+    own = qkv.clone()[:, :Hq * d].unflatten(-1, (Hq, d))
+    hbl.kv_append(cache, k, v, ints(starts), ints(lens), table.cuda(), freqs=freqs, layout=layout, q=own, q_out=own)
+    assert torch.equal(own[:starts[-1]], q_out[:starts[-1]]) and torch.equal(own[starts[-1]:], q[starts[-1]:])
     torch.cuda.synchronize()
     position = torch.zeros(T, dtype=torch.int32)
     where = []
@@ -242,7 +246,7 @@ def test_attention_chunk(hbl, case, d, bits):
 OPTIONS = [
     dict(softcap=30.0), dict(softcap=1.5, scale=0.3), dict(window=1), dict(window=100), dict(slopes=True), dict(prefix_lens=[70, 3, 0]),
     dict(prefix_lens=[1000, 1000, 2], window=50), dict(softcap=20.0, window=333, slopes=True, prefix_lens=[0, 5, 9]), dict(scale=0.0),
-    dict(scale=-0.05)]
+    dict(scale=-0.05), dict(softcap=55.0), dict(slopes=True, prefix_lens=[300, 0, 4], window=120)]
 
 
 @pytest.mark.parametrize("bits,d", [(16, 128), (4, 64), (8, 256), (3, 128)])
@@ -352,6 +356,102 @@ def test_attention_same_bits_every_time(hbl):
     for fill in (0, 255, 127):
         again = hbl.paged_attention(q, cache, *args, workspace=torch.full((n,), fill, dtype=torch.uint8, device="cuda"))
         assert torch.equal(first.view(torch.int16), again.view(torch.int16))
+
+
+MANY = [100, 300]
+
+
+@pytest.mark.parametrize("S", MANY)
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("chunk", [False, True])
+def test_attention_of_many_sequences(hbl, S, bits, chunk):
+    """More sequences than a wave, and than a workgroup, has lanes; empty ones among them."""
+    note(f"attention: {S} sequences bits={bits} chunk={chunk}")
+    new = [(i * 7 % 5 if i % 9 else 40) if chunk else int(i % 10 != 3) for i in range(S)]
+    lens = [n + (i * 37) % 90 for i, n in enumerate(new)]
+    check_attention(hbl, new, lens, 4, 2, 64, bits, 16, seed=S, tail=1)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_attention_with_more_row_tiles_than_are_cut(hbl, bits):
+    note(f"attention: whole row tiles bits={bits}")
+    check_attention(hbl, [1500], [1600], 128, 128, 64, bits, 64, seed=5)
+
+
+@pytest.mark.parametrize("new", [1, 3, 200])
+def test_tokens_beyond_max_q_len_stay(hbl, new):
+    note(f"attention: max_q_len smaller than a sequence's {new}")
+    d, page = 64, 16
+    g = gen(81)
+    lens = [new + 60, 30]
+    table, n = R.page_table(g, lens, page)
+    (kp, _), (vp, _) = (R.random_pages(g, n, 2, page, d, 16, "cuda") for _ in range(2))
+    q = torch.randn((new + 1, 4, d), generator=g).bfloat16().cuda()
+    starts, most = [0, new, new + 1], max(1, new - 2)
+    out = torch.full_like(q, 7.0)
+    hbl.paged_attention(q, hbl.KvCache(kp, vp), ints(starts), ints(lens), table.cuda(), most, out=out)
+    want, bound = R.attention(q, kp, vp, None, None, 16, starts, lens, table.tolist(), d ** -0.5)
+    seen = torch.ones(new + 1, dtype=torch.bool, device="cuda")
+    seen[most:new] = False
+    assert ((out.double() - want).abs() <= bound + (want.abs() + bound) * R.U16 * 1.001)[seen].all() and (out[~seen] == 7.0).all()
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4, 3])
+@pytest.mark.parametrize("new", [1, 70])
+def test_pools_side_by_side_and_beyond_32_bits(hbl, new, bits):
+    """Keys and values of one pool, pages far apart (more than 2^31 values, and bytes, from the first one): as in pools of their own."""
+    note(f"attention: far pages new={new} bits={bits}")
+    d, page, H, n_pages = 256, 64, 2, 4
+    g = gen(91)
+    lens, table = [200], ints([[3, 1, 0, 2]])
+    (kp, ks), (vp, vs) = (R.random_pages(g, n_pages, H, page, d, bits, "cuda") for _ in range(2))
+    q = torch.randn((new, 4, d), generator=g).bfloat16().cuda()
+    k, v = (torch.randn((new, H, d), generator=g).bfloat16().cuda() for _ in range(2))
+    # rows of d * bits / 8 bytes: the last page begins beyond byte 2^32 of the pool (16, 8 bits) or row 2^22 times 3
+    page_rows = ((1 << 32) // 3 // (d * bits // 8) + 64) if bits >= 8 else 1 << 22
+    row = tuple(kp.shape[1:])
+    far = torch.zeros((3 * page_rows + 2 * H * page) * kp.shape[-1], dtype=kp.dtype, device="cuda")
+    width = kp.shape[-1]
+    pools = [far[i * H * page * width:].as_strided((n_pages, *row), (page_rows * width, page * width, width, 1)) for i in (0, 1)]
+    scales = [None, None]
+    if bits != 16:
+        far_scales = torch.zeros(3 * page_rows + 2 * H * page, device="cuda")
+        scales = [far_scales[i * H * page:].as_strided((n_pages, H, page), (page_rows, page, 1)) for i in (0, 1)]
+        for a, b in zip(scales, (ks, vs)):
+            a.copy_(b)
+    for a, b in zip(pools, (kp, vp)):
+        a.copy_(b)
+    batch = (ints([0, new]), ints(lens), table)
+    near, apart = hbl.KvCache(kp, vp, bits, ks, vs), hbl.KvCache(*pools, bits, *scales)
+    freqs = hbl.rope_frequencies(128)
+    for cache in (near, apart):
+        hbl.kv_append(cache, k, v, *batch, freqs=freqs)
+    got = [hbl.paged_attention(q, c, *batch, new) for c in (near, apart)]
+    assert torch.equal(got[0].view(torch.int16), got[1].view(torch.int16))
+    assert torch.equal(pools[0].contiguous().view(torch.uint8), kp.view(torch.uint8)) and torch.equal(pools[1].contiguous().view(torch.uint8), vp.view(torch.uint8))
+
+
+def test_chunks_in_a_graph(hbl):
+    """A captured chunk whose keys are cut into parts, replayed at other lengths with eager work between."""
+    note("chunks in a graph")
+    d, page, n, H = 128, 64, 100, 2
+    g = gen(95)
+    table, n_pages = R.page_table(g, [6000], page)
+    (kp, ks), (vp, vs) = (R.random_pages(g, n_pages, H, page, d, 4, "cuda") for _ in range(2))
+    cache, q = hbl.KvCache(kp, vp, 4, ks, vs), torch.randn((n, 8, d), generator=g).bfloat16().cuda()
+    lens, starts, table = ints([500]), ints([0, n]), table.cuda()
+    workspace = torch.empty(hbl.paged_attention_workspace_bytes(cache, n, 1, 8, n), dtype=torch.uint8, device="cuda")
+    hbl.paged_attention(q, cache, starts, lens, table, n, workspace=workspace)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = hbl.paged_attention(q, cache, starts, lens, table, n, workspace=workspace)
+    for length in (100, 6000, 777, 50, 4096):
+        lens.fill_(length)
+        graph.replay()
+        got = y.clone()
+        want = hbl.paged_attention(q, cache, starts, lens, table, n)
+        torch.cuda.synchronize()
+        assert torch.equal(got.view(torch.int16), want.view(torch.int16))
 
 
 # --- together ---------------------------------------------------------------------------------------------------

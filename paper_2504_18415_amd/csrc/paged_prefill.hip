@@ -30,31 +30,32 @@ __device__ __forceinline__ int v_place(int row, int chunk) {
     return row * (2 * D) + ((chunk ^ (D == 64 ? 4 * ((row >> 1) & 1) : 4 * (row & 3))) << 4);
 }
 
+// Row tile `tile` of sequence s.
 struct Item {
-    int s, tile;   // sequence, row tile in it
+    int s, tile;
     SeqSpan span;
     int rows;      // of the sequence (tokens looked at times group)
+    int prefix;
 };
-template <bool UNIFORM = false>
 __device__ __forceinline__ Item item_of(const AttentionArgs& a, int s, int tile) {
-    Item it{s, tile, UNIFORM ? uniform_span(a.batch, a.T, s) : span_of(a.batch, a.T, s), 0};
+    Item it{s, tile, span_of(a.batch, a.T, s), 0, a.prefix_lens ? a.prefix_lens[s] : 0};
     it.rows = (it.span.n < a.max_q ? it.span.n : a.max_q) * a.group;
     return it;
 }
-__device__ __forceinline__ int row_tiles(const AttentionArgs& a, int s) { return (item_of(a, s, 0).rows + kRows - 1) / kRows; }
+__device__ __forceinline__ int row_tiles(const Item& it) { return (it.rows + kRows - 1) / kRows; }
 
 // Keys that some row of the tile sees, from a multiple of the tile of keys on.
 struct TileKeys {
     int base, lo, end;   // a multiple of the tile of keys; the first key; behind the last
 };
-__device__ __forceinline__ TileKeys tile_keys(const AttentionArgs& a, const Item& it, int prefix, int tile) {
+__device__ __forceinline__ TileKeys tile_keys(const AttentionArgs& a, const Item& it, int tile) {
     const int before = it.span.total - it.span.n;
     int first = it.tile * kRows / a.group;
     const int last = min((it.tile + 1) * kRows, it.rows) - 1;
     if (first < -before) first = -before;
     if (first > last / a.group) return {0, 0, 0};
-    const KeyRange lo = visible_keys(before + first, it.span.keys, a.window, prefix);
-    const KeyRange hi = visible_keys(before + last / a.group, it.span.keys, a.window, prefix);
+    const KeyRange lo = visible_keys(before + first, it.span.keys, a.window, it.prefix);
+    const KeyRange hi = visible_keys(before + last / a.group, it.span.keys, a.window, it.prefix);
     if (hi.hi <= lo.lo) return {0, 0, 0};
     return {lo.lo & ~(tile - 1), lo.lo, hi.hi};
 }
@@ -63,76 +64,102 @@ __device__ __forceinline__ TileKeys tile_keys(const AttentionArgs& a, const Item
 //
 // With few units there is none for some CUs, and with a few more than the chip holds at once the last ones run alone: the length is the
 // one that takes the shortest time in one round of the chip, or in two.  The lengths, known on the device only, decide; every
-// workgroup looks for it by itself, a candidate a thread.
-constexpr int kMostSplitSeqs = 128, kMostKeyTiles = 1 << 20;
+// workgroup looks for it by itself, a sequence a lane and then a candidate a lane.
+constexpr int kMostCutSeqs = 64, kMostKeyTiles = 1 << 20;
 // Parts of so many tiles of keys at a length: the quotient rounded up, at most 64 (an estimate by floats, the same wherever it is made).
 __device__ __forceinline__ int parts_at(int tiles, int length, float inverse) {
     return tiles <= length ? 1 : min(64, (int)((float)(tiles - 1) * inverse) + 1);
 }
+// `tiles`, `keys`: of the lane's sequence, its row tiles and the last one's tiles of keys.
+__device__ __forceinline__ int part_length(int tiles, int keys, int n_seqs, int heads, int round, int most) {
+    const int lane = threadIdx.x & 63;
+    uint32_t work = (uint32_t)tiles * (uint32_t)min(keys, kMostKeyTiles);   // (at most `most` row tiles' keys: it fits)
+    for (int m = 1; m < 64; m <<= 1) work += (uint32_t)__shfl_xor((int)work, m, 64);
+    int length = 0x7FFFFFFF, least = 0x7FFFFFFF;
+    for (int rounds = 1; rounds <= 2; ++rounds) {
+        // from an even share on in steps of a 16th of it
+        const float share = (float)work * (float)heads / (float)(rounds * round);
+        const int at = max(4, (int)fminf(share * (1.0f + lane * (1.0f / 16.0f)) + 1.0f, 1e9f));
+        const float inverse = 1.0f / (float)at;
+        int units = 0;
+        float longest = 0.0f;   // (in about tiles: sequences without rows have no keys)
+#pragma unroll 2
+        for (int s = 0; s < n_seqs; ++s) {
+            const int t = __builtin_amdgcn_readlane(tiles, s), k = __builtin_amdgcn_readlane(keys, s), parts = parts_at(k, at, inverse);
+            units += t * parts;
+            longest = fmaxf(longest, (float)k * __builtin_amdgcn_rcpf((float)parts));
+        }
+        // (a unit's beginning and end cost about as much as four tiles)
+        int cost = units * heads <= min(rounds * round, most) ? rounds * ((int)fminf(longest, 1e6f) + 4) : 0x7FFFFFFF;
+        const int mine = cost;
+        for (int m = 1; m < 64; m <<= 1) cost = min(cost, __shfl_xor(cost, m, 64));
+        if (cost < least) {
+            least = cost;
+            length = __builtin_amdgcn_readlane(at, 63 - __builtin_clzll(__ballot(mine == cost)));
+        }
+    }
+    return length;
+}
 struct Search {
-    int tiles[kMostSplitSeqs], keys[kMostSplitSeqs];   // of a sequence: row tiles; tiles of keys of the last of them
-    int sums[kWaves], best[2 * kWaves], found[3];
+    int sums[kWaves], found[2];
 };
 struct Unit {
-    int s, tile, part, parts;
-    int all;   // units of a key head
+    Item item;         // item.s < 0: there is none
+    int part, parts;
+    int ordinal, items;   // of the row tile, of all of them (where keys are cut)
 };
-// Unit `rank` of a key head (a function of it, which may need `all`); s < 0: there is none.  `round`: units that run at once, 0: parts are whole.
+// Unit `rank` of a key head (a function of the number of them).  `round`: units that run at once, 0: parts are whole.
 template <typename Rank>
 __device__ __forceinline__ Unit find_unit(const AttentionArgs& a, Search* lds, int tile, int round, int most, Rank rank_of) {
     const int n_seqs = a.batch.n_seqs, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    int length = 0x7FFFFFFF;
-    if (round > 0) {
-        if ((int)threadIdx.x < n_seqs) {
-            const int n = row_tiles(a, threadIdx.x);
-            TileKeys k{0, 0, 0};
-            if (n > 0) k = tile_keys(a, item_of(a, threadIdx.x, n - 1), a.prefix_lens ? a.prefix_lens[threadIdx.x] : 0, tile);
-            lds->tiles[threadIdx.x] = n;
-            lds->keys[threadIdx.x] = (k.end - k.base + tile - 1) / tile;
+    Unit unit{};
+    unit.item.s = -1;
+    unit.parts = 1;
+    if (n_seqs <= kMostCutSeqs) {
+        Item it{};
+        if (lane < n_seqs) it = item_of(a, lane, 0);
+        const int tiles = row_tiles(it);
+        int parts = 1, tiles_upto = tiles;
+        if (round > 0) {
+            it.tile = max(tiles - 1, 0);
+            const TileKeys k = tile_keys(a, it, tile);
+            const int keys = (k.end - k.base + tile - 1) / tile;
+            // (one wave looks for it: with 19 sequences all four took 8 us)
+            if (wave == 0) lds->found[0] = part_length(tiles, keys, n_seqs, a.cache.heads, round, most);
+            __syncthreads();
+            const int length = uniform(lds->found[0]);
+            parts = parts_at(keys, length, 1.0f / (float)length);
         }
-        __syncthreads();
-        uint32_t work = 0;   // (at most `most` row tiles' keys: it fits)
-        for (int s = 0; s < n_seqs; ++s) work += (uint32_t)lds->tiles[s] * (uint32_t)min(lds->keys[s], kMostKeyTiles);
-        // candidates: from an even share of a round (of two) on in steps of a 32nd of it
-        const int rounds = 1 + wave / (kWaves / 2), step = (wave % (kWaves / 2)) * 64 + lane;
-        const float share = (float)work * (float)a.cache.heads / (float)(rounds * round);
-        int at = max(4, (int)fminf(share * (1.0f + step * (1.0f / 32.0f)) + 1.0f, 1e9f));
-        const float inverse = 1.0f / (float)at;
-        int units = 0, longest = 0;
-        for (int s = 0; s < n_seqs; ++s) {
-            const int parts = parts_at(lds->keys[s], at, inverse);
-            units += min(lds->tiles[s] * parts, 1 << 20);
-            longest = max(longest, lds->tiles[s] > 0 ? (int)((float)lds->keys[s] / (float)parts) : 0);
-        }
-        // (a unit's beginning and end cost about as much as four tiles)
-        const bool fits = (int64_t)units * a.cache.heads <= min(rounds * round, most);
-        int cost = fits ? rounds * (longest + 4) : 0x7FFFFFFF;
-        for (int m = 1; m < 64; m <<= 1) {
-            const int c = __shfl_xor(cost, m, 64), l = __shfl_xor(at, m, 64);
-            if (c < cost || (c == cost && l > at)) {
-                cost = c;
-                at = l;
+        int upto = tiles * parts;
+        for (int m = 1; m < n_seqs; m <<= 1) {
+            const int u = __shfl_up(upto, m, 64), v = __shfl_up(tiles_upto, m, 64);
+            if (lane >= m) {
+                upto += u;
+                tiles_upto += v;
             }
         }
-        if (lane == 0) {
-            lds->best[2 * wave] = cost;
-            lds->best[2 * wave + 1] = at;
-        }
-        __syncthreads();
-        int least = 0x7FFFFFFF;
-        for (int w = 0; w < kWaves; ++w)
-            if (lds->best[2 * w] < least) {
-                least = lds->best[2 * w];
-                length = lds->best[2 * w + 1];
-            }
+        const int rank = rank_of(__builtin_amdgcn_readlane(upto, n_seqs - 1));
+        unit.items = __builtin_amdgcn_readlane(tiles_upto, n_seqs - 1);
+        const uint64_t beyond = __ballot(upto > rank);
+        if (rank < 0 || beyond == 0) return unit;
+        const int s = __builtin_ctzll(beyond);
+        unit.parts = __builtin_amdgcn_readlane(parts, s);
+        const int in_seq = rank - __builtin_amdgcn_readlane(upto - tiles * parts, s);
+        unit.item.s = s;
+        unit.item.tile = in_seq / unit.parts;
+        unit.part = in_seq - unit.item.tile * unit.parts;
+        unit.ordinal = __builtin_amdgcn_readlane(tiles_upto - tiles, s) + unit.item.tile;
+        unit.item.span = SeqSpan{__builtin_amdgcn_readlane(it.span.first, s), __builtin_amdgcn_readlane(it.span.n, s),
+                                 __builtin_amdgcn_readlane(it.span.keys, s), __builtin_amdgcn_readlane(it.span.total, s)};
+        unit.item.rows = __builtin_amdgcn_readlane(it.rows, s);
+        unit.item.prefix = __builtin_amdgcn_readlane(it.prefix, s);
+        return unit;
     }
-    // where the sequences' units begin
+    // many sequences: nothing is cut, and a thread has several of them
     const int per = (n_seqs + kThreads - 1) / kThreads;
     const int from = min((int)threadIdx.x * per, n_seqs), to = min(from + per, n_seqs);
-    const float inverse = 1.0f / (float)length;
-    auto parts_of = [&](int s) { return round > 0 ? parts_at(lds->keys[s], length, inverse) : 1; };
     int mine = 0;
-    for (int s = from; s < to; ++s) mine += row_tiles(a, s) * parts_of(s);
+    for (int s = from; s < to; ++s) mine += row_tiles(item_of(a, s, 0));
     int v = mine;
     for (int m = 1; m < 64; m <<= 1) {
         const int u = __shfl_up(v, m, 64);
@@ -141,42 +168,39 @@ __device__ __forceinline__ Unit find_unit(const AttentionArgs& a, Search* lds, i
     if (lane == 63) lds->sums[wave] = v;
     if (threadIdx.x == 0) lds->found[0] = -1;
     __syncthreads();
-    Unit unit{-1, 0, 0, 1, 0};
-    int at = v - mine;
+    int at = v - mine, all = 0;
     for (int w = 0; w < kWaves; ++w) {
         if (w < wave) at += lds->sums[w];
-        unit.all += lds->sums[w];
+        all += lds->sums[w];
     }
-    unit.all = uniform(unit.all);
-    const int rank = rank_of(unit.all);
+    const int rank = rank_of(uniform(all));
     for (int s = from; s < to; ++s) {
-        const int parts = parts_of(s), n = row_tiles(a, s) * parts;
+        const int n = row_tiles(item_of(a, s, 0));
         if (rank >= at && rank < at + n) {
             lds->found[0] = s;
             lds->found[1] = rank - at;
-            lds->found[2] = parts;
         }
         at += n;
     }
     __syncthreads();
-    unit.s = __builtin_amdgcn_readfirstlane(lds->found[0]);
-    unit.parts = __builtin_amdgcn_readfirstlane(lds->found[2]);
-    if (unit.s >= 0) {
-        const int in_seq = __builtin_amdgcn_readfirstlane(lds->found[1]);
-        unit.tile = in_seq / unit.parts;
-        unit.part = in_seq - unit.tile * unit.parts;
+    unit.item.s = uniform(lds->found[0]);
+    if (unit.item.s >= 0) {
+        unit.item.tile = uniform(lds->found[1]);
+        unit.item.span = uniform_span(a.batch, a.T, unit.item.s);
+        unit.item.rows = (unit.item.span.n < a.max_q ? unit.item.span.n : a.max_q) * a.group;
+        unit.item.prefix = a.prefix_lens ? table_entry(a.prefix_lens, unit.item.s) : 0;
     }
     return unit;
 }
 
-// A row tile that was cut, as its first part's workgroup notes it: the slots of its parts are heads apart from `slot` on.
-struct Done {
-    int s, tile, head, slot, parts;
+// What the second launch needs of a row tile and key head: its parts (with one, nothing is to be done) and the slot of the first; the
+// other parts' slots are `heads` apart.
+struct Note {
+    int first, tile, rows, slot, parts;   // first token of the sequence, row tile, rows of the sequence
 };
-// Workspace: outputs [most][kRows][d], maxima and sums [most][kRows], notes [workgroups].
-__device__ __forceinline__ Done* done_of(const AttentionArgs& a, int most) {
-    return reinterpret_cast<Done*>(a.partial + (size_t)most * kRows * (a.d + 2));
-}
+// Workspace: outputs [most][kRows][d], maxima and sums [most][kRows], the number of row tiles, notes [row tile][head].
+__device__ __forceinline__ int* count_of(const AttentionArgs& a, int most) { return reinterpret_cast<int*>(a.partial + (size_t)most * kRows * (a.d + 2)); }
+__device__ __forceinline__ Note* notes_of(const AttentionArgs& a, int most) { return reinterpret_cast<Note*>(count_of(a, most) + 4); }
 
 struct Part {
     int from, to;   // tiles of keys
@@ -220,16 +244,15 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void page
         }
         return rank;
     });
-    const bool mine_at_all = head < heads && unit.s >= 0;
-    // (what this workgroup takes, for the second launch: nothing, or a part of a row tile that is whole where it has one part)
-    if (most > 0 && threadIdx.x == 0)
-        done_of(a, most)[blockIdx.x] = mine_at_all && unit.part == 0 && unit.parts > 1
-                                           ? Done{unit.s, unit.tile, head, rank * heads + head, unit.parts}
-                                           : Done{-1, 0, 0, 0, 0};
-    if (!mine_at_all) return;
-    const Item it = item_of<true>(a, unit.s, unit.tile);
-    const int prefix = a.prefix_lens ? table_entry(a.prefix_lens, it.s) : 0;
-    const TileKeys keys = tile_keys(a, it, prefix, TK);
+    if (most > 0 && threadIdx.x == 0) {
+        if (blockIdx.x == 0) *count_of(a, most) = unit.items;
+        if (head < heads && unit.item.s >= 0 && unit.part == 0)
+            notes_of(a, most)[unit.ordinal * heads + head] =
+                Note{unit.item.span.first, unit.item.tile, unit.item.rows, rank * heads + head, unit.parts};
+    }
+    if (head >= heads || unit.item.s < 0) return;
+    const Item& it = unit.item;
+    const TileKeys keys = tile_keys(a, it, TK);
     const Part mine = part_of((keys.end - keys.base + TK - 1) / TK, unit.part, unit.parts);
     const int32_t* table = a.batch.block_table + it.s * a.batch.table_stride;
 
@@ -237,48 +260,20 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void page
     const int row = it.tile * kRows + wave * 32 + col, token = row / a.group, h = head * a.group + row - token * a.group;
     const bool live = row < it.rows;
     const int position = live ? it.span.total - it.span.n + token : -1;
-    const KeyRange see = visible_keys(position, it.span.keys, a.window, prefix);
+    const KeyRange see = visible_keys(position, it.span.keys, a.window, it.prefix);
     const float slope = SHAPE >= kBiased && a.slopes && live ? a.slopes[h] : 0.0f;
-    bf16x8 q[D / 16];
-    float start = 0.0f;
-    {
-        // (a negative scale turns the queries round: what follows takes a scale of at least 0)
-        const uint32_t sign = a.scale < 0.0f ? 0x80008000u : 0u;
-        const uint16_t* from_q = a.q + (it.span.first + token) * a.q_stride + (int64_t)h * D;
-        float sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (live) x = *reinterpret_cast<const uint4*>(from_q + 16 * i + 8 * half);
-            const uint32_t y[4] = {x.x ^ sign, x.y ^ sign, x.z ^ sign, x.w ^ sign};
-            u32x4 z;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                z[j] = !Codes<BITS>::kPaired ? y[j] : __builtin_amdgcn_perm(y[2 + (j >> 1)], y[j >> 1], (j & 1) ? 0x07060302u : 0x05040100u);
-                if constexpr (CODES) sum += as_f(y[j] << 16) + as_f(y[j] & 0xFFFF0000u);
-            }
-            q[i] = __builtin_bit_cast(bf16x8, z);
-        }
-        if constexpr (CODES) start = -kBias * join32(sum, SumOf());
-    }
     // What a sum of products is multiplied by: to be a score in units of log 2, the exponent of the cap's e^(2 s / cap) in them, a score.
     // Codes get it with their scales.  (At least the smallest normal number: minus infinity, in hidden places, has to stay that.)
     const float cap2 = a.softcap * kLog2e, scale = fabsf(a.scale);
     const float factor = SHAPE == kScaled ? fmaxf(scale * kLog2e, 1.17549435e-38f) : SHAPE == kCapped ? scale * (2.0f * kLog2e / a.softcap) : SHAPE == kBiased ? scale * kLog2e : scale;
     const float step = CODES || SHAPE != kScaled ? 1.0f : factor;
-    // keys that all of the wave's rows see, and those that some does
-    int all_lo = live ? see.lo : 0, all_hi = live ? see.hi : 0x7FFFFFFF, any_lo = see.hi > see.lo ? see.lo : 0x7FFFFFFF, any_hi = see.hi > see.lo ? see.hi : 0;
-    for (int m = 1; m < 32; m <<= 1) {
-        all_lo = max(all_lo, __shfl_xor(all_lo, m, 64));
-        all_hi = min(all_hi, __shfl_xor(all_hi, m, 64));
-        any_lo = min(any_lo, __shfl_xor(any_lo, m, 64));
-        any_hi = max(any_hi, __shfl_xor(any_hi, m, 64));
-    }
-    all_lo = __builtin_amdgcn_readfirstlane(all_lo);
-    all_hi = __builtin_amdgcn_readfirstlane(all_hi);
-    any_lo = __builtin_amdgcn_readfirstlane(any_lo);
-    any_hi = __builtin_amdgcn_readfirstlane(any_hi);
-
+    // keys that all of the wave's rows see, and those that some does: ranges begin and end the later, the later the token
+    const int before = it.span.total - it.span.n, wave_row = it.tile * kRows + wave * 32;
+    const int first_token = wave_row / a.group, last_token = min(wave_row + 31, it.rows - 1) / a.group;
+    const KeyRange first_see = visible_keys(before + first_token, it.span.keys, a.window, it.prefix);
+    const KeyRange last_see = visible_keys(before + last_token, it.span.keys, a.window, it.prefix);
+    const int all_lo = last_see.lo, all_hi = first_see.hi;
+    const int any_lo = first_see.lo, any_hi = wave_row < it.rows ? last_see.hi : 0;
     f32x16 o[D / 32], psum;
 #pragma unroll
     for (int i = 0; i < 16; ++i) psum[i] = 0.0f;
@@ -384,13 +379,34 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void page
         const int key0 = keys.base + mine.from * TK;
         pages = pages_of(key0);
         next_pages = pages_of(key0 + TK);
-        if constexpr (CODES) {
-            fetch_codes(key0, pages);
-            store_codes(0);
-        } else {
-            fetch16(key0, page_at(pages, wave * RW / 16), 0);
-        }
+        if constexpr (CODES) fetch_codes(key0, pages);
+        else fetch16(key0, page_at(pages, wave * RW / 16), 0);
     }
+    // queries, while the first tile is on its way
+    bf16x8 q[D / 16];
+    float start = 0.0f;
+    {
+        // (a negative scale turns the queries round: what follows takes a scale of at least 0)
+        const uint32_t sign = a.scale < 0.0f ? 0x80008000u : 0u;
+        const uint16_t* from_q = a.q + (it.span.first + token) * a.q_stride + (int64_t)h * D;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (live) x = *reinterpret_cast<const uint4*>(from_q + 16 * i + 8 * half);
+            const uint32_t y[4] = {x.x ^ sign, x.y ^ sign, x.z ^ sign, x.w ^ sign};
+            u32x4 z;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                z[j] = !Codes<BITS>::kPaired ? y[j] : __builtin_amdgcn_perm(y[2 + (j >> 1)], y[j >> 1], (j & 1) ? 0x07060302u : 0x05040100u);
+                if constexpr (CODES) sum += as_f(y[j] << 16) + as_f(y[j] & 0xFFFF0000u);
+            }
+            q[i] = __builtin_bit_cast(bf16x8, z);
+        }
+        if constexpr (CODES) start = -kBias * join32(sum, SumOf());
+    }
+    if constexpr (CODES)
+        if (mine.from < mine.to) store_codes(0);
     gemm::wait_loads_then_barrier<0>();
     for (int t = mine.from; t < mine.to; ++t) {
         const int buffer = (t - mine.from) & 1, key0 = keys.base + t * TK;
@@ -567,21 +583,20 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void page
 
 // Joins the parts of a quarter of a row tile (32 rows) of a key head a workgroup.
 __global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(AttentionArgs a, int most) {
-    const int quarter = blockIdx.x & 3, heads = a.cache.heads;
-    const Done unit = done_of(a, most)[blockIdx.x >> 2];
-    if (unit.s < 0) return;
-    const int head = unit.head;
-    const Item it = item_of<true>(a, uniform(unit.s), unit.tile);
+    const int quarter = blockIdx.x & 3, heads = a.cache.heads, index = blockIdx.x >> 2, head = index % heads;
+    if (index >= *count_of(a, most) * heads) return;
+    const Note note = notes_of(a, most)[index];
+    if (note.parts == 1) return;
     const float2* const part_ml = reinterpret_cast<const float2*>(a.partial + (size_t)most * kRows * a.d);
-    const int rows = min(32, it.rows - it.tile * kRows - 32 * quarter);
+    const int rows = min(32, note.rows - note.tile * kRows - 32 * quarter);
     for (int i = threadIdx.x; i < rows * (a.d / 4); i += kThreads) {
-        const int r = 32 * quarter + i / (a.d / 4), at = 4 * (i % (a.d / 4)), row = it.tile * kRows + r;
+        const int r = 32 * quarter + i / (a.d / 4), at = 4 * (i % (a.d / 4)), row = note.tile * kRows + r;
         const int token = row / a.group, h = head * a.group + row - token * a.group;
         float top = -INFINITY, total = 0.0f;
         f32x4 y = {0, 0, 0, 0};
 #pragma unroll 4
-        for (int x = 0; x < unit.parts; ++x) {   // (a part without keys has left -inf, 0 and zeros)
-            const size_t at_row = ((size_t)unit.slot + (size_t)x * heads) * kRows + r;
+        for (int x = 0; x < note.parts; ++x) {   // (a part without keys has left -inf, 0 and zeros)
+            const size_t at_row = ((size_t)note.slot + (size_t)x * heads) * kRows + r;
             const float2 ml = part_ml[at_row];
             const f32x4 o = *reinterpret_cast<const f32x4*>(a.partial + at_row * a.d + at);
             const float to = fmaxf(top, ml.x), ref = to == -INFINITY ? 0.0f : to;
@@ -591,7 +606,7 @@ __global__ __launch_bounds__(kThreads) void paged_prefill_join_kernel(AttentionA
             top = to;
         }
         const float inverse = total > 0.0f ? 1.0f / total : 0.0f;
-        *reinterpret_cast<uint2*>(a.out + (it.span.first + token) * a.out_stride + (int64_t)h * a.d + at) =
+        *reinterpret_cast<uint2*>(a.out + (note.first + token) * a.out_stride + (int64_t)h * a.d + at) =
             make_uint2(pack_bf16(y[0] * inverse, y[1] * inverse), pack_bf16(y[2] * inverse, y[3] * inverse));
     }
 }
@@ -607,7 +622,7 @@ constexpr int round_of(int d) { return d == 256 ? 256 : d == 64 ? 768 : 512; }
 constexpr int most_units(int d) { return d == 256 ? 500 : d == 64 ? 1500 : 1000; }
 // Whether keys are cut: if there may be units for it.
 bool cut_keys(int64_t T, int n_seqs, int group, int heads, int d) {
-    return n_seqs <= kMostSplitSeqs && most_row_tiles(T, n_seqs, group) * heads < most_units(d);
+    return n_seqs <= kMostCutSeqs && most_row_tiles(T, n_seqs, group) * heads < most_units(d);
 }
 
 template <int D, int BITS>
@@ -626,7 +641,7 @@ int launch_form(const AttentionArgs& a, hipStream_t stream) {
     const bool cut = cut_keys(a.T, a.batch.n_seqs, a.group, heads, D);
     const int most = cut ? most_units(D) : 0, round = cut ? round_of(D) : 0;
     // (heads in eights: each XCD has a head's units one after the other, so the grid is whole eights)
-    const int64_t wgs = cut ? (most + 7) / 8 * 8 : most_row_tiles(a.T, a.batch.n_seqs, a.group) * heads;
+    const int64_t tiles = most_row_tiles(a.T, a.batch.n_seqs, a.group), wgs = cut ? (most + 7) / 8 * 8 : tiles * heads;
     if (wgs > 0x7FFFFFFF) return HBL_E_SHAPE;
     int rc;
     if (a.slopes && a.softcap == 0.0f) rc = launch_shape<D, BITS, kBiased>(a, (unsigned)wgs, round, most, stream);
@@ -635,7 +650,7 @@ int launch_form(const AttentionArgs& a, hipStream_t stream) {
     else rc = launch_shape<D, BITS, kScaled>(a, (unsigned)wgs, round, most, stream);
     if (rc != HBL_OK) return rc;
     if (cut)
-        launch_kernel("paged_prefill_join_kernel", paged_prefill_join_kernel, dim3((unsigned)(4 * wgs)), dim3(kThreads), 0, stream, a, most);
+        launch_kernel("paged_prefill_join_kernel", paged_prefill_join_kernel, dim3((unsigned)(4 * tiles * heads)), dim3(kThreads), 0, stream, a, most);
     return after_launch();
 }
 template <int D>
@@ -651,7 +666,7 @@ int launch_bits(const AttentionArgs& a, int bits, hipStream_t stream) {
 }  // namespace
 
 size_t paged_prefill_workspace(int64_t T, int n_seqs, int group, int heads, int d) {
-    return cut_keys(T, n_seqs, group, heads, d) ? (size_t)most_units(d) * kRows * (d + 2) * sizeof(float) + (most_units(d) + 8) * sizeof(Done) : 0;
+    return cut_keys(T, n_seqs, group, heads, d) ? (size_t)most_units(d) * (kRows * (d + 2) * sizeof(float) + sizeof(Note)) + 4 * sizeof(int) : 0;
 }
 
 int launch_paged_prefill(const AttentionArgs& a, int bits, hipStream_t stream) {

@@ -467,13 +467,22 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void page
             }
             const bool plain = key0 >= all_lo && key0 + TK <= all_hi && absent == 0;
             if (!plain) {
+                // (against the lane's own range from its first key of the tile on: constants then)
+                const int lo = see.lo - key0 - 4 * half, hi = see.hi - key0 - 4 * half;
 #pragma unroll
                 for (int b = 0; b < KB; ++b)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const int in_tile = 32 * b + 8 * (i >> 2) + 4 * half + (i & 3), j = key0 + in_tile;
-                        if (j < see.lo || j >= see.hi || (absent >> (2 * b + (i >> 3)) & 1)) score[b][i] = -INFINITY;
+                        const int place = 32 * b + 8 * (i >> 2) + (i & 3);
+                        if (place < lo || place >= hi) score[b][i] = -INFINITY;
                     }
+                if (absent != 0) {
+#pragma unroll
+                    for (int b = 0; b < KB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (absent >> (2 * b + (i >> 3)) & 1) score[b][i] = -INFINITY;
+                }
             }
             float ref = 0.0f;
             if constexpr (SHAPE != kCapped) {

@@ -5,7 +5,7 @@
 // The transposed map (the gradient's) is the same with -angle.  The angle is a product in fp64 reduced to a part of one turn before it
 // becomes fp32: at position 10^6 an fp32 product would be off by 0.03 rad.
 //
-// Memory-bound streaming kernels: every value is read once and written once.  A workgroup first puts the r/2 factors of each of its
+// Memory-bound streaming kernels: every value is read once and written once (6.4 TB/s at 134 MB, 5.4 with fp32).  A workgroup first puts the r/2 factors of each of its
 // tokens into LDS, one per thread (an fp64 product and a sincospif: done per value they would cost as much as the traffic), then its
 // threads take 16 values of a head each: two pieces of 8, the two sides of 8 pairs, so that a rotation needs no other lane.
 #include "hbl_internal.h"
@@ -52,10 +52,18 @@ __device__ __forceinline__ void widen8(const Raw<BF16>& r, float* v) {
         }
     }
 }
-template <bool BF16>
+// STREAM: with the non-temporal hint, so that a launch need not write its output back out of L2 before it ends.  For bf16 outputs that
+// L2 could not hold anyway: smaller ones are read from there by the next launch.  (8192 tokens of 32 heads of 128: 23.4 -> 21.0 us; the
+// queries of an append to 4-bit pages 98 -> 90 with its read-back.  fp32 leaves by halves of a line, which the hint would not join.)
+constexpr int64_t kStreamBytes = (int64_t)32 << 20;
+template <bool BF16, bool STREAM = false>
 __device__ __forceinline__ void store8(void* out, int64_t at, const float* v) {
     if constexpr (BF16) {
-        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at) = pack_bf16x8(v);
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+        const uint4 w = pack_bf16x8(v);
+        u32x4* to = reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + at);
+        if constexpr (STREAM) __builtin_nontemporal_store((u32x4){w.x, w.y, w.z, w.w}, to);
+        else *to = (u32x4){w.x, w.y, w.z, w.w};
     } else {
         float4* p = reinterpret_cast<float4*>(static_cast<float*>(out) + at);
         p[0] = make_float4(v[0], v[1], v[2], v[3]);
@@ -78,30 +86,33 @@ __device__ __forceinline__ float2 turn(const Rotation& r, int position, int i) {
     return make_float2(r.magnitude * c, r.sign * r.magnitude * s);
 }
 
-// Thread j of a head holds the pieces (of 8 values) first and second: in the rotated part the two sides of pairs 8j .. 8j + 7.
+// Thread j of a head's `lanes` holds two pieces, so that neighbours' lie side by side (a load or store of a wave then covers whole
+// lines): of the half layout's rotated part the two sides of pairs 8j .. 8j + 7.  A piece of the interleaved layout has its own four pairs.
 struct Pieces {
     int first, second;
 };
-__device__ __forceinline__ Pieces pieces_of(const Rotation& r, int j) {
-    const int half = r.pairs >> 3;
-    if (!r.interleaved && j < half) return {j, j + half};
-    return {2 * j, 2 * j + 1};
+__device__ __forceinline__ Pieces pieces_of(const Rotation& r, int lanes, int j) {
+    const int half = r.interleaved ? 0 : r.pairs >> 3;
+    return j < half ? Pieces{j, j + half} : Pieces{half + j, lanes + j};   // (the rest from piece 2 half on, its second half lanes - half further)
+}
+__device__ __forceinline__ void rotate_pairs4(const Rotation& r, const float2* turns, int piece, float* v) {
+    if (4 * piece >= r.pairs) return;
+    const float2* t = turns + 4 * piece;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 u = t[i];
+        const float x = v[2 * i], y = v[2 * i + 1];
+        v[2 * i] = x * u.x - y * u.y;
+        v[2 * i + 1] = x * u.y + y * u.x;
+    }
 }
 // (separate products and one rounding each, as the formula is written: codes made of the result do not depend on the call)
-__device__ __forceinline__ void rotate16(const Rotation& r, const float2* turns, int j, float* a, float* b) {
-    if (8 * j >= r.pairs) return;
-    const float2* t = turns + 8 * j;
+__device__ __forceinline__ void rotate16(const Rotation& r, const float2* turns, const Pieces& p, int j, float* a, float* b) {
     if (r.interleaved) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 u = t[i], w = t[4 + i];
-            const float x = a[2 * i], y = a[2 * i + 1], p = b[2 * i], q = b[2 * i + 1];
-            a[2 * i] = x * u.x - y * u.y;
-            a[2 * i + 1] = x * u.y + y * u.x;
-            b[2 * i] = p * w.x - q * w.y;
-            b[2 * i + 1] = p * w.y + q * w.x;
-        }
-    } else {
+        rotate_pairs4(r, turns, p.first, a);
+        rotate_pairs4(r, turns, p.second, b);
+    } else if (8 * j < r.pairs) {
+        const float2* t = turns + 8 * j;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float2 u = t[i];
@@ -123,7 +134,7 @@ struct RopeArgs {
     Rotation rot;
 };
 
-template <bool BF16, bool BF16OUT>
+template <bool BF16, bool BF16OUT, bool STREAM>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
     extern __shared__ float2 turns[];   // [tokens][pairs]
     const int t0 = (int)blockIdx.x * a.tokens;
@@ -136,15 +147,15 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
     const int lanes = a.d >> 4, per_token = a.H * lanes;
     for (int i = threadIdx.x; i < n * per_token; i += kThreads) {
         const int t = i / per_token, in_token = i - t * per_token, h = in_token / lanes, j = in_token - h * lanes;
-        const Pieces p = pieces_of(a.rot, j);
+        const Pieces p = pieces_of(a.rot, lanes, j);
         const int64_t from = (t0 + t) * a.x_stride + h * a.d, to = (t0 + t) * a.out_stride + h * a.d;
         const Raw<BF16> r1 = load8<BF16>(a.x, from + 8 * p.first), r2 = load8<BF16>(a.x, from + 8 * p.second);
         float v[8], w[8];
         widen8<BF16>(r1, v);
         widen8<BF16>(r2, w);
-        rotate16(a.rot, turns + t * a.rot.pairs, j, v, w);
-        store8<BF16OUT>(a.out, to + 8 * p.first, v);
-        store8<BF16OUT>(a.out, to + 8 * p.second, w);
+        rotate16(a.rot, turns + t * a.rot.pairs, p, j, v, w);
+        store8<BF16OUT, STREAM>(a.out, to + 8 * p.first, v);
+        store8<BF16OUT, STREAM>(a.out, to + 8 * p.second, w);
     }
 }
 
@@ -220,7 +231,7 @@ __device__ __forceinline__ void store_state(const PagedCache& c, bool keys, int6
 }
 
 // One token a workgroup row of the grid, its heads (queries, keys, values in this order) over threads and over gridDim.y.
-template <int BITS, bool BF16, bool BF16Q>
+template <int BITS, bool BF16, bool BF16Q, bool STREAM>   // (STREAM: queries)
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a) {
     extern __shared__ float2 turns[];   // [pairs]
     const int t = blockIdx.x;
@@ -242,16 +253,16 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a) {
         h -= is_q ? 0 : (is_k ? a.Hq : a.Hq + heads);
         const void* x = is_q ? a.q : (is_k ? a.k : a.v);
         const int64_t from = (int64_t)t * (is_q ? a.q_stride : (is_k ? a.k_stride : a.v_stride)) + h * a.d;
-        Pieces p = pieces_of(a.rot, j);
+        const Pieces p = pieces_of(a.rot, lanes, j);
         const Raw<BF16> r1 = load8<BF16>(x, from + 8 * p.first), r2 = load8<BF16>(x, from + 8 * p.second);
         float v[8], w[8];
         widen8<BF16>(r1, v);
         widen8<BF16>(r2, w);
-        if (is_q || is_k) rotate16(a.rot, turns, j, v, w);
+        if (is_q || is_k) rotate16(a.rot, turns, p, j, v, w);
         if (is_q) {
             const int64_t to = (int64_t)t * a.q_out_stride + h * a.d;
-            store8<BF16Q>(a.q_out, to + 8 * p.first, v);
-            store8<BF16Q>(a.q_out, to + 8 * p.second, w);
+            store8<BF16Q, STREAM>(a.q_out, to + 8 * p.first, v);
+            store8<BF16Q, STREAM>(a.q_out, to + 8 * p.second, w);
         } else {   // (a row's lanes are all of one kind: they take this branch together)
             store_state<BITS>(a.cache, is_k, slot < 0 ? -1 : slot + ((int64_t)h << a.cache.page_shift), a.d, p, lanes, j, v, w, a.eps);
         }
@@ -273,8 +284,10 @@ int launch_rope(const void* x, int x_dtype, int64_t T, int64_t H, int64_t d, int
     while (a.tokens < 16 && a.tokens * 2 * per_token <= kThreads) a.tokens *= 2;
     const dim3 grid((unsigned)((T + a.tokens - 1) / a.tokens)), block(kThreads);
     const size_t lds = (size_t)a.tokens * a.rot.pairs * sizeof(float2);   // at most 16 KiB
-    const bool bf = x_dtype == HBL_BF16, bfo = out_dtype == HBL_BF16;
-    auto kern = bf ? (bfo ? rope_kernel<true, true> : rope_kernel<true, false>) : (bfo ? rope_kernel<false, true> : rope_kernel<false, false>);
+    const bool bf = x_dtype == HBL_BF16, bfo = out_dtype == HBL_BF16, far = bfo && T * H * d * 2 > kStreamBytes;
+    auto kern = far   ? (bf ? rope_kernel<true, true, true> : rope_kernel<false, true, true>)
+                : bfo ? (bf ? rope_kernel<true, true, false> : rope_kernel<false, true, false>)
+                      : (bf ? rope_kernel<true, false, false> : rope_kernel<false, false, false>);
     launch_kernel("rope_kernel", kern, grid, block, lds, stream, a);
     return after_launch();
 }
@@ -291,10 +304,12 @@ int launch_kv_append(const PagedCache& cache, int bits, int d, const PagedBatch&
     while (parts * T < 512 && parts * kThreads < items) parts *= 2;
     const dim3 grid((unsigned)T, (unsigned)parts), block(kThreads);
     const size_t lds = (size_t)a.rot.pairs * sizeof(float2);
-    const bool bf = x_dtype == HBL_BF16, bfq = q_out_dtype == HBL_BF16;
-#define HBL_APPEND(B)                                                                                              \
-    launch_kernel("kv_append_kernel", bf ? (bfq ? kv_append_kernel<B, true, true> : kv_append_kernel<B, true, false>)   \
-                                         : (bfq ? kv_append_kernel<B, false, true> : kv_append_kernel<B, false, false>), \
+    const bool bf = x_dtype == HBL_BF16, bfq = q_out_dtype == HBL_BF16, far = bfq && T * a.Hq * d * 2 > kStreamBytes;
+#define HBL_APPEND(B)                                                                                                       \
+    launch_kernel("kv_append_kernel",                                                                                       \
+                  far   ? (bf ? kv_append_kernel<B, true, true, true> : kv_append_kernel<B, false, true, true>)             \
+                  : bfq ? (bf ? kv_append_kernel<B, true, true, false> : kv_append_kernel<B, false, true, false>)           \
+                        : (bf ? kv_append_kernel<B, true, false, false> : kv_append_kernel<B, false, false, false>),        \
                   grid, block, lds, stream, a)
     switch (bits) {
         case 16: HBL_APPEND(16); break;

@@ -62,6 +62,20 @@ def test_rope(hbl, T, H, d, rot, extra, dtype, out_dtype, layout):
             assert torch.equal(y[0, :, rot:].float(), x[0, :, rot:].to(out_dtype).float())
 
 
+def test_rope_and_append_of_outputs_beyond_l2(hbl):
+    """Outputs of more than 32 MiB leave by other stores: the same values as in parts that do not."""
+    note("rope and append, large outputs")
+    T, H, d = 5000, 32, 128
+    x = torch.randn((T, H, d), generator=gen(2)).bfloat16().cuda()
+    positions, freqs = torch.arange(T, dtype=torch.int32, device="cuda"), R.frequencies(d).cuda()
+    for layout in ("half", "interleaved"):
+        parts = [hbl.rope(x[i:i + 1000], positions[i:i + 1000], freqs, layout=layout) for i in range(0, T, 1000)]
+        assert torch.equal(hbl.rope(x, positions, freqs, layout=layout).view(torch.int16), torch.cat(parts).view(torch.int16))
+        cache = hbl.KvCache.empty(80, 1, 64, d)
+        q = hbl.kv_append(cache, x[:, :1], x[:, 1:2], ints([0, T]), ints([T]), ints([list(range(80))]), freqs=freqs, layout=layout, q=x)
+        assert torch.equal(q.view(torch.int16), torch.cat(parts).view(torch.int16))
+
+
 def test_rope_in_place_in_a_fused_output(hbl):
     """Queries and keys turned where the projection left them; values and what lies beside untouched."""
     note("rope in place")

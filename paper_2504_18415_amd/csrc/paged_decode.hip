@@ -481,34 +481,56 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void paged_decode_kerne
     }
 }
 
-// Joins the partial results of one (sequence, key head) a workgroup; zeros where there was nothing to see.
+// One place of four features of a row, over its parts.
+struct Joined {
+    float top = -INFINITY, total = 0.0f;
+    f32x4 y = {0, 0, 0, 0};
+    __device__ __forceinline__ void add(float2 ml, f32x4 o) {
+        const float to = fmaxf(top, ml.x), ref = to == -INFINITY ? 0.0f : to;
+        const float keep = __builtin_amdgcn_exp2f(top - ref), f = __builtin_amdgcn_exp2f(ml.x - ref);
+        total = total * keep + f * ml.y;
+        y = y * keep + f * o;
+        top = to;
+    }
+};
+
+// Joins the partial results of one (sequence, key head), rows blockIdx.y, + gridDim.y, ...; zeros where there was nothing to see.
+// SHARED, for many parts: the threads are d/4 places by so many shares of the parts, which are joined through LDS in their order.  (Three
+// contexts of 131000 keys, 8 heads, 12 rows of about 21 parts: a thread for all parts of a place 15 us, this 6; 64 sequences of two
+// parts or so: 4.8 us and 6.3.)
+template <bool SHARED>
 __global__ __launch_bounds__(kThreads) void paged_decode_join_kernel(AttentionArgs a, int pieces, int tile_rows) {
+    __shared__ f32x4 share_o[SHARED ? kThreads : 1];
+    __shared__ float2 share_ml[SHARED ? kThreads : 1];
     const int heads = a.cache.heads, s = blockIdx.x / heads, head = blockIdx.x - s * heads;
     const SeqWork w = seq_work<true>(a, s);
     const int2 held = held_by(a.partial, pieces, tile_rows, a.d)[blockIdx.x];   // (nobody notes anything where there are no tiles)
     const int g0 = w.tiles > 0 ? held.x : 0, g1 = w.tiles > 0 ? held.y : -1;
     if (g0 == g1) return;   // one workgroup had it all
-    const int rows = w.rows_q * a.group;
+    const int rows = w.rows_q * a.group, places = a.d / 4, place = threadIdx.x % places;
+    const int share = threadIdx.x / places, shares = kThreads / places;   // (of the parts, or of the rows)
     const Partial part = partial_of(a.partial, pieces, tile_rows, a.d);
-    for (int i = threadIdx.x; i < rows * (a.d / 4); i += kThreads) {
-        const int row = i / (a.d / 4), at = 4 * (i - row * (a.d / 4));
-        const int token = row / a.group, h = head * a.group + row - token * a.group;
-        float top = -INFINITY, total = 0.0f;
-        f32x4 y = {0, 0, 0, 0};
+    for (int row = SHARED ? blockIdx.y : share; row < rows; row += SHARED ? gridDim.y : shares) {
+        Joined j;
 #pragma unroll 4
-        for (int g = g0; g <= g1; ++g) {
+        for (int g = g0 + (SHARED ? share : 0); g <= g1; g += SHARED ? shares : 1) {
             const size_t at_row = (size_t)(2 * g + (g == g0)) * tile_rows + row;
-            const float2 ml = part.ml[at_row];
-            const f32x4 o = *reinterpret_cast<const f32x4*>(part.o + at_row * a.d + at);
-            const float to = fmaxf(top, ml.x), ref = to == -INFINITY ? 0.0f : to;
-            const float keep = __builtin_amdgcn_exp2f(top - ref), f = __builtin_amdgcn_exp2f(ml.x - ref);
-            total = total * keep + f * ml.y;
-            y = y * keep + f * o;
-            top = to;
+            j.add(part.ml[at_row], *reinterpret_cast<const f32x4*>(part.o + at_row * a.d + 4 * place));
         }
-        const float inverse = total > 0.0f ? 1.0f / total : 0.0f;
-        *reinterpret_cast<uint2*>(a.out + (w.span.first + token) * a.out_stride + (int64_t)h * a.d + at) =
-            make_uint2(pack_bf16(y[0] * inverse, y[1] * inverse), pack_bf16(y[2] * inverse, y[3] * inverse));
+        if (SHARED && g1 > g0) {
+            share_o[threadIdx.x] = j.y;
+            share_ml[threadIdx.x] = make_float2(j.top, j.total);
+            __syncthreads();
+            if (share == 0)
+                for (int x = 1; x < shares; ++x) j.add(share_ml[x * places + place], share_o[x * places + place]);
+            __syncthreads();
+        }
+        if (!SHARED || share == 0) {
+            const float inverse = j.total > 0.0f ? 1.0f / j.total : 0.0f;
+            const int token = row / a.group, h = head * a.group + row - token * a.group;
+            *reinterpret_cast<uint2*>(a.out + (w.span.first + token) * a.out_stride + (int64_t)h * a.d + 4 * place) =
+                make_uint2(pack_bf16(j.y[0] * inverse, j.y[1] * inverse), pack_bf16(j.y[2] * inverse, j.y[3] * inverse));
+        }
     }
 }
 
@@ -518,8 +540,13 @@ int launch_form(const AttentionArgs& a, hipStream_t stream) {
     constexpr int pieces = pieces_of(D, BITS, NR);
     if (int rc = allow_dynamic_lds<&paged_decode_kernel<D, BITS, NR, SHAPED>, lds>(); rc != HBL_OK) return rc;
     launch_kernel("paged_decode_kernel", paged_decode_kernel<D, BITS, NR, SHAPED>, dim3(pieces), dim3(kThreads), lds, stream, a);
-    launch_kernel("paged_decode_join_kernel", paged_decode_join_kernel, dim3((unsigned)a.batch.n_seqs * (unsigned)a.cache.heads), dim3(kThreads), 0,
-                  stream, a, pieces, 16 * NR);
+    // four parts of a (sequence, head) and more, if all are alike: their rows side by side, as long as that fills the chip
+    const int64_t items = (int64_t)a.batch.n_seqs * a.cache.heads, rows = (int64_t)a.max_q * a.group;
+    if (items * 4 <= pieces)
+        launch_kernel("paged_decode_join_kernel", paged_decode_join_kernel<true>, dim3((unsigned)items, (unsigned)(items * rows <= 2048 ? rows : 2048 / items)),
+                      dim3(kThreads), 0, stream, a, pieces, 16 * NR);
+    else
+        launch_kernel("paged_decode_join_kernel", paged_decode_join_kernel<false>, dim3((unsigned)items), dim3(kThreads), 0, stream, a, pieces, 16 * NR);
     return after_launch();
 }
 template <int D, int BITS>

@@ -125,8 +125,8 @@ __device__ __forceinline__ void load_dwords(const void* p, uint32_t* w) {
     for (int i = 0; i < N; ++i) w[i] = c.w[i];
 }
 
-// An entry of the block table at an index that is the same for the whole wave, by a scalar load: it does not wait in line with the
-// vector loads in flight, as a vector load's result does (those of states that the next tile needs: 670 us were 690 for it).
+// An entry of an index array at a place that is the same for the whole wave, by a scalar load: it does not wait in line behind the vector
+// loads in flight, as a vector load's result does (those of the next tile: an 8192-token prompt of 32 heads 669 -> 637 us).
 __device__ __forceinline__ int table_entry(const int32_t* table, int i) {
     typedef const __attribute__((address_space(4))) int32_t* constant_int;
     return ((constant_int)(uintptr_t)table)[__builtin_amdgcn_readfirstlane(i)];

@@ -358,7 +358,7 @@ int hbl_rope(const void* x, int x_dtype, int64_t T, int64_t H, int64_t d, int64_
  * A paged cache: two pools (keys and values) of n_pages pages of page_size slots.  Row (page p, head h, slot i) of a pool is
  * row p * page_rows + h * page_size + i: d bf16 values (bits == 16), or d codes of 8, 4 or 3 bits as hbl_kv_quant_absmax
  * writes them, with the row's scale at the same index of the scales.  hbl_kv_dequant reads a pool back.
- *   k, v                device, 16-byte aligned;  k_scales, v_scales device fp32 (not read when bits == 16)
+ *   k, v                device, 16-byte aligned (of no pages: not read, may be NULL);  k_scales, v_scales device fp32 (not read when bits == 16)
  *   page_size           a power of two, 16 to 1024
  *   page_rows           rows between two pages, >= n_kv_heads * page_size (more where pools are interleaved)
  *   d                   64, 128 or 256
@@ -416,6 +416,7 @@ int hbl_kv_append(const hbl_kv_cache* cache, const hbl_kv_batch* batch, const vo
  *   q, out          [T, n_q_heads, d] bf16 with strides in values as for hbl_rope; they must not overlap
  *   max_q_len       at least the new tokens of any sequence (those beyond it are left as they were)
  *   sizes           T n_q_heads < 2^31, n_seqs n_kv_heads (table_width page_size + 256) < 2^38
+ *   softcap         0 (none), or 1e-6 and more
  *   window >= 0;  slopes device [n_q_heads] fp32 or NULL;  prefix_lens device [n_seqs] int32 or NULL
  *   workspace       device, >= hbl_paged_attention_workspace_bytes(same arguments), 256-byte aligned; nothing in it has to
  *                   start at a value; calls that may overlap need one each

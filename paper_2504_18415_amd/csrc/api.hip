@@ -564,6 +564,7 @@ int check_cache(const hbl_kv_cache* c) {
     return HBL_OK;
 }
 int check_cache_memory(const hbl_kv_cache* c) {
+    if (c->n_pages == 0) return HBL_OK;   // nothing is read or written there
     if (!c->k || !c->v || (c->bits != 16 && (!c->k_scales || !c->v_scales))) return HBL_E_NULL;
     return aligned16(c->k) && aligned16(c->v) ? HBL_OK : HBL_E_ALIGN;
 }
@@ -673,11 +674,13 @@ int hbl_paged_attention(const void* q, int64_t T, int64_t n_q_heads, int64_t q_s
                         void* stream) {
     int rc = check_attention_shape(cache, batch, T, n_q_heads, max_q_len);
     if (rc != HBL_OK) return rc;
-    if (window < 0 || window > 0x7FFFFFFF || !(softcap >= 0.0f) || std::isinf(softcap) || !std::isfinite(scale)) return HBL_E_SHAPE;
+    if (window < 0 || window > 0x7FFFFFFF || !std::isfinite(scale)) return HBL_E_SHAPE;
+    if (!(softcap == 0.0f || softcap >= 1e-6f) || std::isinf(softcap)) return HBL_E_SHAPE;
     if (T == 0 || batch->n_seqs == 0) return HBL_OK;
     if ((rc = check_cache_memory(cache)) != HBL_OK || (rc = check_batch_memory(batch)) != HBL_OK) return rc;
     if ((rc = check_heads(q, HBL_BF16, T, n_q_heads, cache->d, q_stride)) != HBL_OK) return rc;
     if ((rc = check_heads(out, HBL_BF16, T, n_q_heads, cache->d, out_stride)) != HBL_OK) return rc;
+    if (q == out) return HBL_E_SHAPE;   // (queries are read by several workgroups, and after the first of them has written)
     if (!workspace) return HBL_E_NULL;
     if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return HBL_E_ALIGN;
     if (workspace_bytes < hbl_paged_attention_workspace_bytes(cache, batch, T, n_q_heads, max_q_len)) return HBL_E_WORKSPACE;

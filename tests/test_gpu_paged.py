@@ -644,8 +644,7 @@ def test_empty_calls(hbl):
     assert (out == 7.0).all()
     none, narrow = hbl.KvCache.empty(0, 2, 16, 64), torch.zeros((1, 0), dtype=torch.int32, device="cuda")
     for c, t in ((none, torch.zeros((1, 3), dtype=torch.int32, device="cuda")), (cache, narrow)):
-        if c.n_pages:
-            hbl.kv_append(c, y, y, ints([0, 3]), ints([3]), t)
-            for n in (3, 40):
-                out = hbl.paged_attention(y, c, ints([0, 3]), ints([3]), t, n)
-                assert (out == 0).all()
+        hbl.kv_append(c, y, y, ints([0, 3]), ints([3]), t)
+        assert (hbl.paged_attention(y, c, ints([0, 3]), ints([3]), t, 3) == 0).all()
+        wide = torch.ones((50, 2, 64), dtype=torch.bfloat16, device="cuda")   # (a chunk)
+        assert (hbl.paged_attention(wide, c, ints([0, 50]), ints([50]), t, 50) == 0).all()

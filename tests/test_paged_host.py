@@ -135,7 +135,7 @@ def test_refusals_before_any_launch(hbl):
     def attend(c=None, b=None, q=ok, T=4, Hq=8, qs=512, m=1, scale=0.1, cap=0.0, window=0, out=ctypes.c_void_p(1 << 20), os_=512, ws=ok, wb=1 << 40):
         return L.hbl_paged_attention(q, T, Hq, qs, B(c or cache()), B(b or batch()), m, scale, cap, window, None, None, out, os_, ws, wb, None)
 
-    for kw, want in shapes + [(dict(b=batch(n_seqs=1 << 20, table_width=1 << 14, table_stride=1 << 14)), S), (dict(T=1 << 24, Hq=128, qs=8192, os_=8192), S), (dict(Hq=6), S), (dict(Hq=0), S), (dict(m=0), S), (dict(window=-1), S), (dict(window=1 << 31), S), (dict(cap=-1.0), S),
+    for kw, want in shapes + [(dict(b=batch(n_seqs=1 << 20, table_width=1 << 14, table_stride=1 << 14)), S), (dict(T=1 << 24, Hq=128, qs=8192, os_=8192), S), (dict(Hq=6), S), (dict(Hq=0), S), (dict(m=0), S), (dict(window=-1), S), (dict(window=1 << 31), S), (dict(cap=-1.0), S), (dict(cap=1e-7), S), (dict(out=ok), S),
                               (dict(cap=float("nan")), S), (dict(cap=float("inf")), S), (dict(scale=float("nan")), S), (dict(scale=float("inf")), S),
                               (dict(q=null), N), (dict(out=null), N), (dict(ws=null), N), (dict(qs=511), S), (dict(os_=516), A),
                               (dict(q=ctypes.c_void_p(4097)), A), (dict(ws=ctypes.c_void_p(4096 + 128)), A), (dict(wb=16), hbl.E_WORKSPACE)]:
